@@ -55,6 +55,7 @@ typedef enum specvlm_dtype {
 #define SPECVLM_ERR_TREE_NOT_CLOSED 64 /* draft growth: a chosen candidate whose parent was not chosen */
 
 #define SPECVLM_MAX_NODES 64
+#define SPECVLM_MAX_CHUNK 65536      /* new tokens of a request in one call (specvlm_kv_append, _kv_read, _chunk_attn) */
 #define SPECVLM_PAGE_SIZE 16
 #define SPECVLM_MAX_SPLITS 64        /* key-range splits per (request, head) */
 #define SPECVLM_COUNTER_STRIDE 32              /* int32 words between the arrival counters of two requests */
@@ -467,6 +468,114 @@ int32_t specvlm_draft_finalize(int32_t B, int32_t C, int32_t N_max, const float 
                                const int32_t *root_token_dev, int32_t *parent_out_dev,
                                int32_t *draft_tok_out_dev, int32_t *node_cand_out_dev,
                                int32_t *num_nodes_out_dev, int32_t *err_flag_dev, void *stream);
+
+/*
+ * ---- The cache around the verification: filling it, eight bits, attention of token chunks ----------
+ * Sec. 3.1 / 3.2: the target's cache is filled chunk by chunk (visual and text tokens of the prompt, then
+ * the tokens of a request that has no draft, one at a time) and is streamed from HBM once per step.  The
+ * calls below write new rows into a cache, keep it in eight bits, and attend over it.
+ *
+ * An e4m3 cache holds K and V rows as OCP e4m3 codes (1 byte per element) and one scale per (slot, KV
+ * head), a power of two 2^e stored as the byte e + 127:
+ *     e       = the smallest whole number, -100 at least, with max_d |x_d| <= 448 * 2^e  (finite entries)
+ *     code_d  = x_d * 2^-e rounded to the nearest e4m3 number, ties to the even one; an infinity or NaN
+ *               becomes a NaN code (with e = 120 codes stop at 240: 256 * 2^120 is no float)
+ *     value_d = code_d * 2^e, exact in bfloat16 and fp32
+ * Scaling by a power of two rounds nothing, so the codes do not depend on who computes them.  Geometry: desc's
+ * kv_stride_* count elements (bytes) of the e4m3 cache, multiples of 16; scales are [B, H_kv, kv_capacity]
+ * (paged: [num_blocks, H_kv, 16]) bytes, the slots of a head adjacent.  specvlm_attn_desc.dtype is the type
+ * of the rows outside the cache (new rows, queries, outputs).
+ */
+typedef struct specvlm_kv_scales {
+    uint8_t *k_dev, *v_dev;        /* K's and V's scale bytes */
+    int64_t stride_b, stride_h;    /* bytes from one request (paged: block) / KV head to the next */
+} specvlm_kv_scales;
+
+/*
+ * New rows into the cache, before the attention call that reads them:
+ *     slot prefix_len[b] + i of request b, KV head h  <-  (k|v)_new[b,i,h,:]      i < num_new[b]
+ * as they are (scales NULL: the cache has desc->dtype), or quantised as above.  No other slot is written, rows
+ * i >= num_new[b] are not read.  num_new[b] may be 0; outside [0, N_max] it sets SPECVLM_ERR_BAD_NUM_NODES, slots that the
+ * cache does not have set SPECVLM_ERR_BAD_LENGTH, and the request writes nothing; rows whose block id is
+ * outside [0, num_blocks) are not written and set SPECVLM_ERR_BAD_BLOCK.  Rows at a tree node's slot are
+ * written in node order (slot prefix_len + node), as specvlm_tree_verify_attn wants them.
+ *   desc           dtype, B, N_max (1 .. SPECVLM_MAX_CHUNK), H_kv, D, paged geometry, kv_* are used
+ *   k_new_dev, v_new_dev  device, desc->dtype, element (b,i,h,d) at b*new_stride_b + i*new_stride_n +
+ *                  h*new_stride_h + d (views of a fused projection buffer are fine); rows 16-byte aligned
+ *   num_new_dev    device int32 [B], or NULL meaning N_max for every request
+ *   scales         host struct (read during the call) or NULL
+ */
+int32_t specvlm_kv_append(const specvlm_attn_desc *desc, const void *k_new_dev, const void *v_new_dev,
+                          int64_t new_stride_b, int64_t new_stride_n, int64_t new_stride_h,
+                          const int32_t *num_new_dev, const int32_t *prefix_len_dev,
+                          const int32_t *block_table_dev, void *k_cache_dev, void *v_cache_dev,
+                          const specvlm_kv_scales *scales, int32_t *err_flag_dev, void *stream);
+
+/*
+ * Slots of the cache as dense rows, the inverse of specvlm_kv_append (values of an e4m3 cache, rounded to
+ * desc->dtype, which rounds nothing):
+ *     (k|v)_out[b,i,h,:]  <-  slot start[b] + i of request b, KV head h           i < count[b]
+ * Rows i >= count[b] are left as they were.  start NULL means 0, count NULL means N_max.  Errors as in
+ * specvlm_kv_append (rows whose block id is out of range are left as they were).  Strides as new_stride_*.
+ */
+int32_t specvlm_kv_read(const specvlm_attn_desc *desc, const void *k_cache_dev, const void *v_cache_dev,
+                        const specvlm_kv_scales *scales, const int32_t *start_dev, const int32_t *count_dev,
+                        const int32_t *block_table_dev, void *k_out_dev, void *v_out_dev,
+                        int64_t out_stride_b, int64_t out_stride_n, int64_t out_stride_h,
+                        int32_t *err_flag_dev, void *stream);
+
+/*
+ * specvlm_kv_compact for an e4m3 cache: the accepted path's codes and scales.  Arguments, results and errors
+ * as there; scales->k_dev / v_dev are layer 0's (ignored with layer pointers), scale_layer_stride the bytes
+ * to the next layer's, k_scale_layer_ptrs_dev / v_scale_layer_ptrs_dev device arrays of L device pointers
+ * that go with k_layer_ptrs_dev / v_layer_ptrs_dev.  desc->dtype is not used.
+ */
+int32_t specvlm_kv_compact_quantized(const specvlm_attn_desc *desc, int32_t L,
+                                     void *k_base_dev, void *v_base_dev, int64_t layer_stride,
+                                     void *const *k_layer_ptrs_dev, void *const *v_layer_ptrs_dev,
+                                     const specvlm_kv_scales *scales, int64_t scale_layer_stride,
+                                     void *const *k_scale_layer_ptrs_dev, void *const *v_scale_layer_ptrs_dev,
+                                     const int32_t *block_table_dev, const int32_t *prefix_len_dev,
+                                     const int32_t *path_dev, int32_t path_cap, const int32_t *accept_len_dev,
+                                     int32_t *new_prefix_len_dev, int32_t *moved_idx_dev,
+                                     int32_t *err_flag_dev, void *stream);
+
+/*
+ * Attention of each request's new tokens over the cache that already holds them (specvlm_kv_append), for ONE
+ * layer.  For request b, query head h and new token i < num_new[b]:
+ *     J(i) = {0 .. prefix_len[b] + i}                                                  (parent NULL)
+ *     J(i) = {0 .. prefix_len[b]-1} U {prefix_len[b] + j : j is i or an ancestor of i} (parent given)
+ *     o[b,i,h,:] = softmax_{j in J(i)}(scale * q[b,i,h,:] . K[b,kv(h),j,:]) . V[b,kv(h),j,:]
+ *     lse[b,h,i] = natural-log-sum-exp of the scaled scores over J(i)   (optional)
+ * One token per request (decoding), thousands (a chunk of the prompt), or a draft tree of up to 64 nodes
+ * over an e4m3 cache.  Rows i >= num_new[b] of o / lse are left as they were.  num_new[b] may be 0.
+ * Slots at or beyond prefix_len[b]+num_new[b] are not read.  K of a token that a row does not see may be
+ * anything; V of the request's visible tokens must be finite for every row that sees them, and V of a new
+ * token must be finite (its weight in the rows before it is zero).  Products of bf16 operands (e4m3 values
+ * are exact in bf16), fp32 sums and softmax statistics, weights rounded to bf16 for the second product.
+ *   desc           dtype SPECVLM_BF16 (SPECVLM_F32: SPECVLM_UNSUPPORTED); N_max 1 .. SPECVLM_MAX_CHUNK, with
+ *                  parent 1 .. SPECVLM_MAX_NODES; num_splits 0 lets the library divide the keys, 1 forbids it
+ *                  (anything else: SPECVLM_INVALID_ARG); group = H_q / H_kv with group * (group * N_max + 256) < 2^31
+ *   q_dev, o_dev   device bf16, strides from desc, 16-byte aligned rows
+ *   scales         host struct (e4m3 cache), or NULL (bf16 cache)
+ *   num_new_dev    device int32 [B], or NULL meaning N_max for every request
+ *   parent_dev     device int32 [B, N_max] (a request's tree, rules as above), or NULL
+ *   lse_dev        device fp32 [B, H_q, N_max] or NULL
+ *   workspace_dev  device, 256-byte aligned, ZERO-FILLED ONCE after allocation (every call leaves its counters
+ *                  zero), reusable for every later call whatever its shape; calls that may run concurrently need
+ *                  separate ones.  specvlm_chunk_attn_workspace_bytes(desc), which is never more than
+ *                  SPECVLM_CHUNK_WORKSPACE_BYTES, is what the division of the keys wants; with less (or NULL
+ *                  and 0) the call divides them less, or not at all
+ *   err_flag_dev   SPECVLM_ERR_BAD_NUM_NODES (num_new outside [0, N_max]), BAD_LENGTH, BAD_PARENT: the request's
+ *                  rows are left as they were; BAD_BLOCK: they are unspecified (memory outside the pool is not touched)
+ */
+#define SPECVLM_CHUNK_WORKSPACE_BYTES (64u << 20)
+size_t specvlm_chunk_attn_workspace_bytes(const specvlm_attn_desc *desc);
+int32_t specvlm_chunk_attn(const specvlm_attn_desc *desc, const void *q_dev, const void *k_cache_dev,
+                           const void *v_cache_dev, const specvlm_kv_scales *scales,
+                           const int32_t *block_table_dev, const int32_t *prefix_len_dev,
+                           const int32_t *num_new_dev, const int32_t *parent_dev, void *o_dev, float *lse_dev,
+                           void *workspace_dev, size_t workspace_bytes, int32_t *err_flag_dev, void *stream);
 
 #ifdef __cplusplus
 }

@@ -35,7 +35,8 @@ EXPORTS = ["specvlm_version", "specvlm_last_hip_error", "specvlm_tree_verify_att
            "specvlm_draft_finalize",
            "specvlm_head_argmax", "specvlm_head_argmax_workspace_bytes",
            "specvlm_visual_pool", "specvlm_visual_prune", "specvlm_visual_pool_padded", "specvlm_visual_prune_padded",
-           "specvlm_node_argmax_accept"]
+           "specvlm_node_argmax_accept", "specvlm_kv_append", "specvlm_kv_read", "specvlm_kv_compact_quantized",
+           "specvlm_chunk_attn", "specvlm_chunk_attn_workspace_bytes"]
 
 
 class SpecvlmError(RuntimeError):
@@ -53,6 +54,11 @@ class AttnDesc(ctypes.Structure):
                 ("q_stride_b", ctypes.c_int64), ("q_stride_n", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
                 ("o_stride_b", ctypes.c_int64), ("o_stride_n", ctypes.c_int64), ("o_stride_h", ctypes.c_int64),
                 ("kv_stride_b", ctypes.c_int64), ("kv_stride_h", ctypes.c_int64), ("kv_stride_t", ctypes.c_int64)]
+
+
+class KvScales(ctypes.Structure):
+    """Mirror of specvlm_kv_scales."""
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
 
 
 class _NotLoaded:
@@ -139,6 +145,17 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     L.specvlm_visual_prune_padded.argtypes = L.specvlm_visual_prune.argtypes
     L.specvlm_node_argmax_accept.restype = i32
     L.specvlm_node_argmax_accept.argtypes = [i32] * 5 + [vp, i64, i64] + [vp] * 11
+    desc, scales = ctypes.POINTER(AttnDesc), ctypes.POINTER(KvScales)
+    L.specvlm_kv_append.restype = i32
+    L.specvlm_kv_append.argtypes = [desc, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, scales, vp, vp]
+    L.specvlm_kv_read.restype = i32
+    L.specvlm_kv_read.argtypes = [desc, vp, vp, scales, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp]
+    L.specvlm_kv_compact_quantized.restype = i32
+    L.specvlm_kv_compact_quantized.argtypes = [desc, i32, vp, vp, i64, vp, vp, scales, i64, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    L.specvlm_chunk_attn_workspace_bytes.restype = ctypes.c_size_t
+    L.specvlm_chunk_attn_workspace_bytes.argtypes = [desc]
+    L.specvlm_chunk_attn.restype = i32
+    L.specvlm_chunk_attn.argtypes = [desc, vp, vp, vp, scales, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp]
     _load_native(L)
     _lib = L
     return L
@@ -156,6 +173,7 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"bfloat16 or float32 expected, got {t.dtype}")
 
 
+CHUNK_WORKSPACE_BYTES = 64 << 20    # SPECVLM_CHUNK_WORKSPACE_BYTES: a workspace that specvlm_chunk_attn wants no more of, whatever the shape
 COUNTER_STRIDE = 32                 # SPECVLM_COUNTER_STRIDE: int32 words between two requests' arrival counters
 
 
@@ -313,3 +331,41 @@ def specvlm_node_argmax_accept(logits, parent, draft_tok, *, num_nodes=None, pat
     [B * COUNTER_STRIDE] device tensor, zero-filled once (allocated here when omitted).
     Returns (amax, accept_len, path, bonus_tok, committed_tok)."""
     return _native.node_argmax_accept(logits, parent, draft_tok, num_nodes, path_cap, counters, amax, err_flag, out, stream)
+
+
+def specvlm_kv_append(k_new, v_new, k_cache, v_cache, prefix_len, *, num_new=None, block_table=None, scales=None, err_flag=None,
+                      stream=None):
+    """New rows [B,N,H_kv,D] (bf16 or fp32; may be views of a fused projection buffer) into slots prefix_len[b] .. of the cache, in
+    place.  A cache of the rows' type takes them as they are; a torch.float8_e4m3fn cache takes codes and
+    `scales` = (k_scale, v_scale), uint8 [B,H_kv,capacity] or [num_blocks,H_kv,16], the exponent bytes."""
+    return _native.kv_append(k_new, v_new, k_cache, v_cache, prefix_len, num_new, block_table, scales, err_flag, stream)
+
+
+def specvlm_kv_read(k_cache, v_cache, count, N_max=None, *, start=None, block_table=None, scales=None, out=None, dtype=None,
+                    err_flag=None, stream=None):
+    """Slots start[b] .. start[b] + count[b] - 1 (start: 0) of the cache as dense rows (k, v) [B,N_max,H_kv,D].  `out` = (k, v) supplies
+    them and keeps its rows past count; new ones hold zeros there, and have `dtype` (an e4m3 cache: bfloat16 when omitted)."""
+    like = None if dtype is None else torch.empty(0, dtype=dtype)
+    return _native.kv_read(k_cache, v_cache, count, N_max, start, block_table, scales, out, err_flag, like, stream)
+
+
+def specvlm_kv_compact_quantized(k_caches, v_caches, scales, prefix_len, path, accept_len, *, block_table=None, new_prefix_len=None,
+                                 moved_idx=None, layer_ptrs=None, err_flag=None, stream=None):
+    """specvlm_kv_compact for float8_e4m3fn caches [L, <per-layer dims>] with scales = (k_scale, v_scale), uint8 [L, ...]; or one
+    layer's tensors for the geometry beside layer_ptrs = (k, v, k_scale, v_scale), int64 device tensors of L addresses.
+    Returns (new_prefix_len, moved_idx)."""
+    return _native.kv_compact_quantized(k_caches, v_caches, scales, prefix_len, path, accept_len, block_table, new_prefix_len,
+                                        moved_idx, layer_ptrs, err_flag, stream)
+
+
+def specvlm_chunk_attn_workspace_bytes(desc: AttnDesc) -> int:
+    return int(lib().specvlm_chunk_attn_workspace_bytes(ctypes.byref(desc)))
+
+
+def specvlm_chunk_attn(q, k_cache, v_cache, prefix_len, *, num_new=None, parent=None, block_table=None, scales=None, out=None, lse=None,
+                       workspace=None, err_flag=None, softmax_scale=0.0, num_splits=0, stream=None):
+    """Attention of new tokens q [B,N,H_q,D] over a cache that holds them already (specvlm_kv_append), for one layer: causal, or a draft
+    tree given by `parent` [B,N].  bf16 cache, or float8_e4m3fn with `scales`.  `workspace`: a zero-filled uint8 device tensor kept for
+    calls of any shape (CHUNK_WORKSPACE_BYTES is always enough; allocated here when omitted).  Returns `out` ([B,N,H_q,D])."""
+    return _native.chunk_attn(q, k_cache, v_cache, prefix_len, num_new, parent, block_table, scales, out, lse, workspace, err_flag,
+                              softmax_scale, num_splits, stream)

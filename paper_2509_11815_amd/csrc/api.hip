@@ -12,10 +12,10 @@ void note_hip_error(hipError_t e) { g_last_hip_error = static_cast<int32_t>(e); 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Geometry checks common to attention and compaction.
-static int32_t check_kv_geometry(const specvlm_attn_desc& d) {
-    if (d.dtype != SPECVLM_BF16 && d.dtype != SPECVLM_F32) return SPECVLM_INVALID_ARG;
+static int32_t check_kv_geometry(const specvlm_attn_desc& d, bool quantised = false) {
+    if (!quantised && d.dtype != SPECVLM_BF16 && d.dtype != SPECVLM_F32) return SPECVLM_INVALID_ARG;
     if (d.B < 1 || d.H_kv < 1 || (d.D != 64 && d.D != 128)) return SPECVLM_INVALID_ARG;
-    const int vec = d.dtype == SPECVLM_BF16 ? 8 : 4;                 // elements per 16 bytes
+    const int vec = quantised ? 16 : d.dtype == SPECVLM_BF16 ? 8 : 4;          // elements per 16 bytes
     if (d.kv_stride_t < d.D || d.kv_stride_t % vec || d.kv_stride_h % vec || d.kv_stride_b % vec)
         return SPECVLM_INVALID_ARG;
     if (d.kv_stride_h < 0 || d.kv_stride_b < 0) return SPECVLM_INVALID_ARG;
@@ -50,7 +50,7 @@ using namespace specvlm;
 
 extern "C" {
 
-int32_t specvlm_version(void) { return 300; }
+int32_t specvlm_version(void) { return 400; }
 
 int32_t specvlm_last_hip_error(void) { return g_last_hip_error; }
 
@@ -230,9 +230,122 @@ int32_t specvlm_kv_compact(const specvlm_attn_desc* desc, int32_t L, void* k_bas
         if (layer_stride < 0 || layer_stride % vec) return SPECVLM_INVALID_ARG;
     }
     return launch_kv_compact(*desc, L, k_base_dev, v_base_dev, layer_stride, k_layer_ptrs_dev,
-                             v_layer_ptrs_dev, block_table_dev, prefix_len_dev, path_dev, path_cap,
+                             v_layer_ptrs_dev, nullptr, 0, nullptr, nullptr, block_table_dev, prefix_len_dev, path_dev, path_cap,
                              accept_len_dev, new_prefix_len_dev, moved_idx_dev, err_flag_dev,
                              static_cast<hipStream_t>(stream));
+}
+
+// The scales of an e4m3 cache: bytes, so any alignment does.
+static bool scales_ok(const specvlm_kv_scales& s, bool pointers) {
+    return (!pointers || (s.k_dev && s.v_dev)) && s.stride_b >= 0 && s.stride_h >= 0;
+}
+
+int32_t specvlm_kv_compact_quantized(const specvlm_attn_desc* desc, int32_t L, void* k_base_dev, void* v_base_dev,
+                                     int64_t layer_stride, void* const* k_layer_ptrs_dev, void* const* v_layer_ptrs_dev,
+                                     const specvlm_kv_scales* scales, int64_t scale_layer_stride,
+                                     void* const* k_scale_layer_ptrs_dev, void* const* v_scale_layer_ptrs_dev,
+                                     const int32_t* block_table_dev, const int32_t* prefix_len_dev,
+                                     const int32_t* path_dev, int32_t path_cap, const int32_t* accept_len_dev,
+                                     int32_t* new_prefix_len_dev, int32_t* moved_idx_dev, int32_t* err_flag_dev,
+                                     void* stream) {
+    if (!desc || !scales) return SPECVLM_INVALID_ARG;
+    int32_t rc = check_kv_geometry(*desc, true);
+    if (rc) return rc;
+    if (L < 1 || L > 32767 || desc->H_kv > 65535 || desc->B > 65535) return SPECVLM_INVALID_ARG;
+    if (path_cap < 1 || path_cap > SPECVLM_MAX_NODES) return SPECVLM_INVALID_ARG;
+    if (!prefix_len_dev || !path_dev || !accept_len_dev || !new_prefix_len_dev) return SPECVLM_INVALID_ARG;
+    if ((desc->paged != 0) != (block_table_dev != nullptr)) return SPECVLM_INVALID_ARG;
+    const int by_ptr = !!k_layer_ptrs_dev + !!v_layer_ptrs_dev + !!k_scale_layer_ptrs_dev + !!v_scale_layer_ptrs_dev;
+    if ((by_ptr && by_ptr != 4) || !scales_ok(*scales, !by_ptr)) return SPECVLM_INVALID_ARG;
+    if (!by_ptr) {
+        if (!k_base_dev || !v_base_dev || !aligned16(k_base_dev) || !aligned16(v_base_dev)) return SPECVLM_INVALID_ARG;
+        if (layer_stride < 0 || layer_stride % 16 || scale_layer_stride < 0) return SPECVLM_INVALID_ARG;
+    }
+    return launch_kv_compact(*desc, L, k_base_dev, v_base_dev, layer_stride, k_layer_ptrs_dev, v_layer_ptrs_dev, scales,
+                             scale_layer_stride, k_scale_layer_ptrs_dev, v_scale_layer_ptrs_dev, block_table_dev,
+                             prefix_len_dev, path_dev, path_cap, accept_len_dev, new_prefix_len_dev, moved_idx_dev,
+                             err_flag_dev, static_cast<hipStream_t>(stream));
+}
+
+// New rows into the cache, or cached rows out: what the two calls have in common.
+static int32_t kv_rows(const specvlm_attn_desc* desc, bool append, void* k_cache_dev, void* v_cache_dev,
+                       const specvlm_kv_scales* scales, void* k_rows_dev, void* v_rows_dev, int64_t stride_b,
+                       int64_t stride_n, int64_t stride_h, const int32_t* first_dev, const int32_t* count_dev,
+                       const int32_t* block_table_dev, int32_t* err_flag_dev, void* stream) {
+    if (!desc || (desc->dtype != SPECVLM_BF16 && desc->dtype != SPECVLM_F32)) return SPECVLM_INVALID_ARG;
+    int32_t rc = check_kv_geometry(*desc, scales != nullptr);
+    if (rc) return rc;
+    if (desc->N_max < 1 || desc->N_max > SPECVLM_MAX_CHUNK || desc->B > 65535 || desc->H_kv > 65535) return SPECVLM_INVALID_ARG;
+    if ((desc->paged != 0) != (block_table_dev != nullptr)) return SPECVLM_INVALID_ARG;
+    if (!k_cache_dev || !v_cache_dev || !k_rows_dev || !v_rows_dev || !aligned16(k_cache_dev) || !aligned16(v_cache_dev) ||
+        !aligned16(k_rows_dev) || !aligned16(v_rows_dev))
+        return SPECVLM_INVALID_ARG;
+    const int vec = desc->dtype == SPECVLM_BF16 ? 8 : 4;
+    if (stride_b < 0 || stride_n < 0 || stride_h < desc->D || stride_b % vec || stride_n % vec || stride_h % vec) return SPECVLM_INVALID_ARG;
+    if (scales && !scales_ok(*scales, true)) return SPECVLM_INVALID_ARG;
+    return launch_kv_rows(*desc, append, k_cache_dev, v_cache_dev, scales, k_rows_dev, v_rows_dev, stride_b, stride_n, stride_h,
+                          first_dev, count_dev, block_table_dev, err_flag_dev, static_cast<hipStream_t>(stream));
+}
+
+int32_t specvlm_kv_append(const specvlm_attn_desc* desc, const void* k_new_dev, const void* v_new_dev, int64_t new_stride_b,
+                          int64_t new_stride_n, int64_t new_stride_h, const int32_t* num_new_dev, const int32_t* prefix_len_dev,
+                          const int32_t* block_table_dev, void* k_cache_dev, void* v_cache_dev, const specvlm_kv_scales* scales,
+                          int32_t* err_flag_dev, void* stream) {
+    if (!prefix_len_dev) return SPECVLM_INVALID_ARG;
+    return kv_rows(desc, true, k_cache_dev, v_cache_dev, scales, const_cast<void*>(k_new_dev), const_cast<void*>(v_new_dev), new_stride_b,
+                   new_stride_n, new_stride_h, prefix_len_dev, num_new_dev, block_table_dev, err_flag_dev, stream);
+}
+
+int32_t specvlm_kv_read(const specvlm_attn_desc* desc, const void* k_cache_dev, const void* v_cache_dev,
+                        const specvlm_kv_scales* scales, const int32_t* start_dev, const int32_t* count_dev,
+                        const int32_t* block_table_dev, void* k_out_dev, void* v_out_dev, int64_t out_stride_b,
+                        int64_t out_stride_n, int64_t out_stride_h, int32_t* err_flag_dev, void* stream) {
+    return kv_rows(desc, false, const_cast<void*>(k_cache_dev), const_cast<void*>(v_cache_dev), scales, k_out_dev, v_out_dev, out_stride_b,
+                   out_stride_n, out_stride_h, start_dev, count_dev, block_table_dev, err_flag_dev, stream);
+}
+
+static int32_t check_chunk_desc(const specvlm_attn_desc& d, bool quantised, bool tree) {
+    if (d.dtype == SPECVLM_F32) return SPECVLM_UNSUPPORTED;
+    if (d.dtype != SPECVLM_BF16) return SPECVLM_INVALID_ARG;
+    int32_t rc = check_kv_geometry(d, quantised);
+    if (rc) return rc;
+    if (d.H_q < 1 || d.H_q % d.H_kv || d.B > 65535) return SPECVLM_INVALID_ARG;
+    if (d.N_max < 1 || d.N_max > (tree ? SPECVLM_MAX_NODES : SPECVLM_MAX_CHUNK)) return SPECVLM_INVALID_ARG;
+    const int64_t group = d.H_q / d.H_kv;
+    if (group * (group * d.N_max + 256) >= (int64_t{1} << 31)) return SPECVLM_INVALID_ARG;       // row -> token by a 32-bit reciprocal
+    if (!(d.softmax_scale >= 0.f) || isinf(d.softmax_scale)) return SPECVLM_INVALID_ARG;
+    if (d.num_splits < 0 || d.num_splits > 1) return SPECVLM_INVALID_ARG;
+    const int64_t st[6] = {d.q_stride_b, d.q_stride_n, d.q_stride_h, d.o_stride_b, d.o_stride_n, d.o_stride_h};
+    for (int64_t s : st)
+        if (s < 0 || s % 8) return SPECVLM_INVALID_ARG;
+    if (d.q_stride_h < d.D || d.o_stride_h < d.D) return SPECVLM_INVALID_ARG;
+    return SPECVLM_OK;
+}
+
+size_t specvlm_chunk_attn_workspace_bytes(const specvlm_attn_desc* desc) {
+    return desc && !check_chunk_desc(*desc, false, false) ? chunk_workspace_bytes(*desc) : 0;      // (either kind of cache)
+}
+
+int32_t specvlm_chunk_attn(const specvlm_attn_desc* desc, const void* q_dev, const void* k_cache_dev, const void* v_cache_dev,
+                           const specvlm_kv_scales* scales, const int32_t* block_table_dev, const int32_t* prefix_len_dev,
+                           const int32_t* num_new_dev, const int32_t* parent_dev, void* o_dev, float* lse_dev,
+                           void* workspace_dev, size_t workspace_bytes, int32_t* err_flag_dev, void* stream) {
+    if (!desc) return SPECVLM_INVALID_ARG;
+    int32_t rc = check_chunk_desc(*desc, scales != nullptr, parent_dev != nullptr);
+    if (rc) return rc;
+    if (!q_dev || !k_cache_dev || !v_cache_dev || !prefix_len_dev || !o_dev) return SPECVLM_INVALID_ARG;
+    if ((desc->paged != 0) != (block_table_dev != nullptr)) return SPECVLM_INVALID_ARG;
+    if (!aligned16(q_dev) || !aligned16(k_cache_dev) || !aligned16(v_cache_dev) || !aligned16(o_dev)) return SPECVLM_INVALID_ARG;
+    if (scales && !scales_ok(*scales, true)) return SPECVLM_INVALID_ARG;
+    if (workspace_dev && (reinterpret_cast<uintptr_t>(workspace_dev) & 255u)) return SPECVLM_INVALID_ARG;
+    ChunkArgs a;
+    a.d = *desc;
+    a.scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / sqrtf(static_cast<float>(desc->D));
+    a.q = q_dev; a.k = k_cache_dev; a.v = v_cache_dev; a.scales = scales; a.block_table = block_table_dev;
+    a.prefix_len = prefix_len_dev; a.num_new = num_new_dev; a.parent = parent_dev; a.o = o_dev; a.lse = lse_dev;
+    a.workspace = workspace_dev; a.workspace_bytes = workspace_dev ? workspace_bytes : 0;
+    a.err_flag = err_flag_dev; a.stream = static_cast<hipStream_t>(stream);
+    return launch_chunk_attn(a);
 }
 
 static bool rows_ok(int32_t dtype, int32_t E, const void* p, int64_t sb, int64_t st) {

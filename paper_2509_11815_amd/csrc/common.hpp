@@ -72,9 +72,15 @@ int32_t launch_tree_accept_sample(int32_t dtype, int32_t B, int32_t N_max, int32
 
 int32_t launch_kv_compact(const specvlm_attn_desc& d, int32_t L, void* k_base, void* v_base,
                           int64_t layer_stride, void* const* k_ptrs, void* const* v_ptrs,
-                          const int32_t* block_table, const int32_t* prefix_len, const int32_t* path,
+                          const specvlm_kv_scales* scales, int64_t scale_layer_stride, void* const* ks_ptrs,
+                          void* const* vs_ptrs, const int32_t* block_table, const int32_t* prefix_len, const int32_t* path,
                           int32_t path_cap, const int32_t* accept_len, int32_t* new_prefix_len,
                           int32_t* moved_idx, int32_t* err_flag, hipStream_t stream);
+
+// Rows into the cache (append) or out of it; `first` slots, `count` rows per request.
+int32_t launch_kv_rows(const specvlm_attn_desc& d, bool append, void* k_cache, void* v_cache, const specvlm_kv_scales* scales,
+                       void* k_rows, void* v_rows, int64_t stride_b, int64_t stride_n, int64_t stride_h, const int32_t* first,
+                       const int32_t* count, const int32_t* block_table, int32_t* err_flag, hipStream_t stream);
 
 int32_t launch_visual_pool(int32_t dtype, int32_t B, int32_t T, int32_t E, int32_t ratio, const void* x,
                            int64_t x_sb, int64_t x_st, const int32_t* num_tokens, void* y, int64_t y_sb,
@@ -136,5 +142,26 @@ int32_t launch_attn_wave(const AttnArgs& a);
 int32_t launch_attn_streams(const AttnArgs& a);
 // Device address of the current device's library-owned scratch array (SPECVLM_STATIC_WORKSPACE_BYTES).
 int32_t attn_static_workspace(void** ptr_out);
+
+struct ChunkArgs {
+    specvlm_attn_desc d;
+    float scale;                // resolved softmax scale
+    const void* q;
+    const void* k;
+    const void* v;
+    const specvlm_kv_scales* scales;      // e4m3 cache, else nullptr
+    const int32_t* block_table;
+    const int32_t* prefix_len;
+    const int32_t* num_new;
+    const int32_t* parent;
+    void* o;
+    float* lse;
+    void* workspace;            // nullptr where there is none to use
+    size_t workspace_bytes;
+    int32_t* err_flag;
+    hipStream_t stream;
+};
+size_t chunk_workspace_bytes(const specvlm_attn_desc& d);
+int32_t launch_chunk_attn(const ChunkArgs& a);
 
 }  // namespace specvlm

@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -30,7 +31,8 @@ namespace {
     X(specvlm_tree_accept) X(specvlm_node_argmax_accept) X(specvlm_tree_accept_sample) X(specvlm_kv_compact) \
     X(specvlm_draft_topk) X(specvlm_draft_topk_select) X(specvlm_draft_select) X(specvlm_draft_finalize)   \
     X(specvlm_head_argmax_workspace_bytes) X(specvlm_head_argmax) X(specvlm_visual_pool) X(specvlm_visual_prune)  \
-    X(specvlm_visual_pool_padded) X(specvlm_visual_prune_padded)
+    X(specvlm_visual_pool_padded) X(specvlm_visual_prune_padded) X(specvlm_kv_append) X(specvlm_kv_read)   \
+    X(specvlm_kv_compact_quantized) X(specvlm_chunk_attn) X(specvlm_chunk_attn_workspace_bytes)
 #define SPECVLM_DECLARE(name) decltype(&::name) name;
 struct Entries { SPECVLM_NATIVE_ENTRIES(SPECVLM_DECLARE) } lib;
 #undef SPECVLM_DECLARE
@@ -653,6 +655,231 @@ PyObject* visual_prune(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the cache around the verification --------------------------------------------------------------
+// A device tensor of `like`'s device (a host pointer in a kernel would end the process).
+const at::Tensor& on_device(const Arguments& a, int i, const char* name, const at::Tensor& like) {
+    const at::Tensor& t = a.tensor(i, name);
+    if (!t.is_cuda() || t.device() != like.device()) fail(PyExc_TypeError, "%s must be a device tensor of the call's device", name);
+    return t;
+}
+// An int32 device tensor of n entries, or None
+int32_t* per_request(const Arguments& a, int i, const char* name, const at::Tensor& like, int64_t n) {
+    if (!a.given(i)) return nullptr;
+    int32_t* p = a.i32(i, name);
+    if (on_device(a, i, name, like).numel() < n) fail(PyExc_ValueError, "%s has too few entries", name);
+    return p;
+}
+int32_t* error_word(const Arguments& a, int i, const at::Tensor& like) { return per_request(a, i, "err_flag", like, 1); }
+
+// K and V cache (first: index of K's argument, V's behind it) with their block table and scales: geometry and pointers.  `skip`: leading
+// dimensions (layers).  e4m3 caches come with scales, others without.
+struct Cache {
+    const at::Tensor &k, &v;
+    specvlm_attn_desc d{};
+    specvlm_kv_scales scales{};
+    const specvlm_kv_scales* scales_given = nullptr;
+    int64_t scale_layer_stride = 0;
+    int32_t* table = nullptr;
+    Cache(const Arguments& a, int first, int table_arg, int scales_arg, const at::Tensor& like, int64_t B, int skip = 0)
+        : k(on_device(a, first, "k_cache", like)), v(on_device(a, first + 1, "v_cache", like)) {
+        want(k.dim() == 4 + skip, "the caches must have four dimensions a layer");
+        want(k.strides() == v.strides() && k.sizes() == v.sizes() && k.scalar_type() == v.scalar_type(), "K and V caches must share one geometry");
+        want(k.stride(3 + skip) == 1, "innermost dimension must be contiguous");
+        d.B = B; d.H_kv = k.size(skip + 1); d.D = k.size(skip + 3);
+        d.kv_stride_b = k.stride(skip); d.kv_stride_h = k.stride(skip + 1); d.kv_stride_t = k.stride(skip + 2);
+        d.kv_capacity = k.size(skip + 2);
+        if (a.given(table_arg)) {
+            const at::Tensor& t = on_device(a, table_arg, "block_table", like);
+            want(t.dim() == 2 && t.size(0) == B, "block_table must be [B, blocks]");
+            table = a.i32(table_arg, "block_table");
+            d.paged = 1;
+            d.block_size = k.size(skip + 2);
+            d.max_blocks_per_req = t.size(1);
+            d.num_blocks = k.size(skip);
+            d.kv_capacity = d.max_blocks_per_req * d.block_size;
+        } else {
+            want(k.size(skip) == B, "a contiguous cache has a row per request");
+        }
+        const bool e4m3 = k.scalar_type() == at::kFloat8_e4m3fn;
+        want(e4m3 == a.given(scales_arg), "a float8_e4m3fn cache comes with scales, any other without");
+        if (!e4m3) return;
+        THPObjectPtr pair(PySequence_Fast(a.obj(scales_arg), "scales must be (k_scale, v_scale)"));
+        if (!pair) throw python_error();
+        want(PySequence_Fast_GET_SIZE(pair.get()) == 2, "scales must be (k_scale, v_scale)");
+        PyObject** const item = PySequence_Fast_ITEMS(pair.get());
+        const Arguments both{item, 2, a.what};
+        const at::Tensor &ks = on_device(both, 0, "k_scale", like), &vs = on_device(both, 1, "v_scale", like);
+        want(ks.scalar_type() == at::kByte && vs.scalar_type() == at::kByte, "scales must be uint8 tensors");
+        want(ks.dim() == 3 + skip && ks.sizes() == k.sizes().slice(0, 3 + skip) && ks.stride(2 + skip) == 1 && ks.strides() == vs.strides() &&
+             ks.sizes() == vs.sizes(), "scales must have the caches' leading dimensions, the slots adjacent, and one geometry");
+        scales = {static_cast<uint8_t*>(ks.data_ptr()), static_cast<uint8_t*>(vs.data_ptr()), ks.stride(skip), ks.stride(skip + 1)};
+        scales_given = &scales;
+        if (skip) scale_layer_stride = ks.stride(0);
+    }
+};
+
+// Dense K and V rows [B, N, H_kv, D] of one geometry.
+void dense_rows(const at::Tensor& k, const at::Tensor& v, const Cache& c) {
+    want(k.dim() == 4 && k.sizes() == v.sizes() && k.strides() == v.strides() && k.scalar_type() == v.scalar_type(), "K and V rows must share one geometry [B, N, H_kv, D]");
+    want(k.size(2) == c.d.H_kv && k.size(3) == c.d.D && k.stride(3) == 1, "K and V rows must be [B, N, H_kv, D] with D contiguous");
+    want(c.scales_given || k.scalar_type() == c.k.scalar_type(), "rows and cache must have one type");
+}
+
+// (k_new, v_new, k_cache, v_cache, prefix_len, num_new, block_table, scales, err_flag, stream)
+PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    const Arguments a{args, nargs, "specvlm_kv_append"};
+    const at::Tensor& k = on_device(a, 0, "k_new", a.tensor(0, "k_new"));
+    const at::Tensor& v = on_device(a, 1, "v_new", k);
+    const c10::hip::HIPGuard device(k.device().index());
+    const CallStream on(a, 9, k);
+    want(k.dim() == 4, "K and V rows must share one geometry [B, N, H_kv, D]");
+    const int64_t B = k.size(0);
+    Cache c(a, 2, 6, 7, k, B);
+    dense_rows(k, v, c);
+    c.d.dtype = dtype_code(k);
+    c.d.N_max = k.size(1);
+    check(unlocked(lib.specvlm_kv_append, &c.d, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                   per_request(a, 5, "num_new", k, B), per_request(a, 4, "prefix_len", k, B), c.table, c.k.data_ptr(), c.v.data_ptr(),
+                   c.scales_given, error_word(a, 8, k), on.handle()),
+          a.what);
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// (k_cache, v_cache, count, N_max, start, block_table, scales, out, err_flag, dtype_like, stream): dtype_like: an (empty) tensor of the type
+// wanted, or None
+PyObject* kv_read(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    const Arguments a{args, nargs, "specvlm_kv_read"};
+    const at::Tensor& like = on_device(a, 0, "k_cache", a.tensor(0, "k_cache"));
+    const at::Tensor& count = on_device(a, 2, "count", like);
+    const c10::hip::HIPGuard device(like.device().index());
+    const CallStream on(a, 10, like);
+    const int64_t B = count.numel();
+    Cache c(a, 0, 5, 6, like, B);
+    at::Tensor k, v;
+    THPObjectPtr pair;
+    PyObject *given_k = Py_None, *given_v = Py_None;
+    if (a.given(7)) {
+        pair = PySequence_Fast(a.obj(7), "out must be (k, v)");
+        if (!pair) throw python_error();
+        want(PySequence_Fast_GET_SIZE(pair.get()) == 2, "out must be (k, v)");
+        PyObject** const item = PySequence_Fast_ITEMS(pair.get());
+        const Arguments both{item, 2, a.what};
+        k = on_device(both, 0, "out", like);
+        v = on_device(both, 1, "out", like);
+        given_k = item[0];
+        given_v = item[1];
+        want(k.dim() == 4 && k.size(0) == B, "out must be two tensors [B, N, H_kv, D]");
+    } else {
+        want(a.given(3), "N_max or out must be given");
+        const auto type = a.given(9) ? a.tensor(9, "dtype").scalar_type() : c.scales_given ? at::kBFloat16 : c.k.scalar_type();
+        k = at::zeros({B, a.as_int(3), c.d.H_kv, c.d.D}, like.options().dtype(type));       // rows past count are not written
+        v = at::zeros_like(k);
+    }
+    dense_rows(k, v, c);
+    c.d.dtype = dtype_code(k);
+    c.d.N_max = k.size(1);
+    check(unlocked(lib.specvlm_kv_read, &c.d, c.k.data_ptr(), c.v.data_ptr(), c.scales_given, per_request(a, 4, "start", like, B),
+                   per_request(a, 2, "count", like, B), c.table, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                   error_word(a, 8, like), on.handle()),
+          a.what);
+    return tuple_of<2>({on.keep(given_k, k), on.keep(given_v, v)});
+    END_HANDLE_TH_ERRORS
+}
+
+// (k_caches, v_caches, scales, prefix_len, path, accept_len, block_table, new_prefix_len, moved_idx, layer_ptrs, err_flag, stream)
+PyObject* kv_compact_quantized(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    const Arguments a{args, nargs, "specvlm_kv_compact_quantized"};
+    const at::Tensor& path = a.tensor(4, "path");
+    on_device(a, 4, "path", path);
+    want(path.dim() == 2, "path must have two dimensions");
+    const c10::hip::HIPGuard device(path.device().index());
+    const CallStream on(a, 11, path);
+    const int64_t B = path.size(0), cap = path.size(1);
+    const bool by_ptr = a.given(9);
+    Cache c(a, 0, 6, 2, path, B, by_ptr ? 0 : 1);
+    want(c.scales_given, "k_caches must be float8_e4m3fn tensors");
+    void* const* ptrs[4] = {nullptr, nullptr, nullptr, nullptr};
+    int64_t L = by_ptr ? 0 : c.k.size(0);
+    if (by_ptr) {
+        THPObjectPtr four(PySequence_Fast(a.obj(9), "layer_ptrs must be (k, v, k_scale, v_scale)"));
+        if (!four) throw python_error();
+        want(PySequence_Fast_GET_SIZE(four.get()) == 4, "layer_ptrs must be (k, v, k_scale, v_scale)");
+        const Arguments each{PySequence_Fast_ITEMS(four.get()), 4, a.what};
+        for (int x = 0; x < 4; ++x) {
+            const at::Tensor& t = on_device(each, x, "layer_ptrs", path);
+            want(t.scalar_type() == at::kLong && t.is_contiguous() && (x == 0 || t.numel() == L), "layer_ptrs must be int64 tensors of one length");
+            L = t.numel();
+            ptrs[x] = static_cast<void* const*>(t.data_ptr());
+        }
+    }
+    at::Tensor made;
+    if (!a.given(7)) made = new_i32(path, {B});
+    int32_t* new_prefix = a.given(7) ? per_request(a, 7, "new_prefix_len", path, B) : static_cast<int32_t*>(made.data_ptr());
+    check(unlocked(lib.specvlm_kv_compact_quantized, &c.d, static_cast<int32_t>(L), by_ptr ? nullptr : c.k.data_ptr(),
+                   by_ptr ? nullptr : c.v.data_ptr(), by_ptr ? int64_t{0} : c.k.stride(0), ptrs[0], ptrs[1], c.scales_given,
+                   c.scale_layer_stride, ptrs[2], ptrs[3], c.table, per_request(a, 3, "prefix_len", path, B), a.i32(4, "path"),
+                   static_cast<int32_t>(cap), per_request(a, 5, "accept_len", path, B), new_prefix,
+                   per_request(a, 8, "moved_idx", path, B * cap * 2), error_word(a, 10, path), on.handle()),
+          a.what);
+    Py_INCREF(a.obj(8));
+    return tuple_of<2>({on.keep(a.obj(7), made), a.obj(8)});
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, k_cache, v_cache, prefix_len, num_new, parent, block_table, scales, out, lse, workspace, err_flag, softmax_scale, num_splits, stream)
+PyObject* chunk_attn(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    const Arguments a{args, nargs, "specvlm_chunk_attn"};
+    const at::Tensor& q = on_device(a, 0, "q", a.tensor(0, "q"));
+    const c10::hip::HIPGuard device(q.device().index());
+    const CallStream on(a, 14, q);
+    want(q.dim() == 4 && q.stride(3) == 1, "q must be [B, N, H_q, D] with D contiguous");
+    const int64_t B = q.size(0), N = q.size(1), H = q.size(2);
+    Cache c(a, 1, 6, 7, q, B);
+    want(q.size(3) == c.d.D, "q and the caches must have one head size");
+    want(c.scales_given || c.k.scalar_type() == q.scalar_type(), "q and a cache without scales must have one type");
+    at::Tensor made;
+    if (!a.given(8)) made = at::zeros(q.sizes(), q.options());       // rows past num_new are not written
+    const at::Tensor& out = a.given(8) ? on_device(a, 8, "out", q) : made;
+    want(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type() && out.stride(3) == 1, "out must have q's shape and type, D contiguous");
+    specvlm_attn_desc& d = c.d;
+    d.dtype = dtype_code(q);
+    d.N_max = N; d.H_q = H;
+    d.softmax_scale = a.as_float(12);
+    d.num_splits = static_cast<int32_t>(a.as_int(13));
+    d.q_stride_b = q.stride(0); d.q_stride_n = q.stride(1); d.q_stride_h = q.stride(2);
+    d.o_stride_b = out.stride(0); d.o_stride_n = out.stride(1); d.o_stride_h = out.stride(2);
+    float* lse = nullptr;
+    if (a.given(9)) {
+        const at::Tensor& t = on_device(a, 9, "lse", q);
+        want(t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == B * H * N, "lse must be a contiguous float32 tensor [B, H_q, N]");
+        lse = static_cast<float*>(t.data_ptr());
+    }
+    const int32_t* parent = per_request(a, 5, "parent", q, B * N);
+    void* ws = nullptr;
+    size_t bytes = 0;
+    at::Tensor scratch;                              // (of the call's stream: may be given back as soon as the call is enqueued)
+    if (a.given(10)) {
+        const at::Tensor& t = on_device(a, 10, "workspace", q);
+        want(t.is_contiguous(), "workspace must be contiguous");
+        ws = t.data_ptr();
+        bytes = t.numel() * t.element_size();
+    } else if ((bytes = lib.specvlm_chunk_attn_workspace_bytes(&d)) != 0) {
+        scratch = at::zeros({static_cast<int64_t>(bytes)}, q.options().dtype(at::kByte));
+        ws = scratch.data_ptr();
+    }
+    check(unlocked(lib.specvlm_chunk_attn, &d, q.data_ptr(), c.k.data_ptr(), c.v.data_ptr(), c.scales_given, c.table,
+                   per_request(a, 3, "prefix_len", q, B), per_request(a, 4, "num_new", q, B), parent, out.data_ptr(), lse, ws, bytes,
+                   error_word(a, 11, q), on.handle()),
+          a.what);
+    return on.keep(a.obj(8), made);
+    END_HANDLE_TH_ERRORS
+}
+
 // bind({entry point: address}, SpecvlmError)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
@@ -682,6 +909,7 @@ PyMethodDef methods[] = {
     SPECVLM_METHOD(tree_accept), SPECVLM_METHOD(node_argmax_accept), SPECVLM_METHOD(tree_accept_sample),
     SPECVLM_METHOD(draft_topk), SPECVLM_METHOD(draft_topk_select), SPECVLM_METHOD(draft_select), SPECVLM_METHOD(draft_finalize),
     SPECVLM_METHOD(head_argmax), SPECVLM_METHOD(visual_pool), SPECVLM_METHOD(visual_prune),
+    SPECVLM_METHOD(kv_append), SPECVLM_METHOD(kv_read), SPECVLM_METHOD(kv_compact_quantized), SPECVLM_METHOD(chunk_attn),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_specvlm_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -311,10 +311,18 @@ int32_t launch_tree_accept(int32_t B, int32_t N_max, int32_t path_cap, const int
 // do not move (path[j] == j, always true for the root) are skipped.
 // A workgroup's few loads and stores are one chain of latencies, so with many of them it is their number that
 // counts: 32 layers x 8 requests x 32 heads with a workgroup per head (16384) 13.8 us, 2048 of them 4.0 (compact_plan.hpp).
+// QUANTISED: the lane that has a row's first chunk moves the row's scale byte as well.
 // ---------------------------------------------------------------------------------------
+struct CompactScales {
+    unsigned char *k_base, *v_base;
+    int64_t layer_stride, stride_b, stride_h;
+    void *const *k_ptrs, *const *v_ptrs;
+};
+
+template <bool QUANTISED>
 __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(
     KvGeom g, unsigned char* k_base, unsigned char* v_base, int64_t layer_stride_bytes,
-    void* const* k_ptrs, void* const* v_ptrs, int elem_bytes, int chunk_bits, int head_bits, int H_kv,
+    void* const* k_ptrs, void* const* v_ptrs, CompactScales scales, int elem_bytes, int chunk_bits, int head_bits, int H_kv,
     const int32_t* __restrict__ prefix_len, const int32_t* __restrict__ path, int path_cap,
     const int32_t* __restrict__ accept_len, int32_t* __restrict__ new_prefix_len, int32_t* __restrict__ moved_idx,
     int32_t* __restrict__ err_flag) {
@@ -350,8 +358,20 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(
     const int m = min(max(accept_len[b], 0), path_cap - 1);
     uint4 regs[kCompactChunksPerThread];
     int64_t dst_off[kCompactChunksPerThread];
+    unsigned char* s_base = nullptr;
+    KvGeom sg = g;
+    int scale_of[kCompactChunksPerThread];
+    int64_t scale_to[kCompactChunksPerThread];
+    if constexpr (QUANTISED) {
+        s_base = scales.k_ptrs ? static_cast<unsigned char*>(which ? scales.v_ptrs[l] : scales.k_ptrs[l])
+                               : (which ? scales.v_base : scales.k_base) + l * scales.layer_stride;
+        sg.stride_b = scales.stride_b;
+        sg.stride_h = scales.stride_h;
+        sg.stride_t = 1;
+    }
 #pragma unroll
     for (int c = 0; c < kCompactChunksPerThread; ++c) {
+        if constexpr (QUANTISED) scale_to[c] = -1;
         const int idx = tid + c * kCompactThreads;
         const int ch = idx & ((1 << chunk_bits) - 1), hk = hk0 + ((idx >> chunk_bits) & ((1 << head_bits) - 1));
         const int j = idx >> bits;
@@ -366,6 +386,12 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(
             if (!bad_block) {                      // a row whose block id is out of range stays where it is
                 regs[c] = *reinterpret_cast<const uint4*>(base + src);
                 dst_off[c] = dst;
+                if constexpr (QUANTISED) {
+                    if (ch == 0) {
+                        scale_of[c] = s_base[kv_row_offset(sg, b, hk, P + a[c], bad_block)];
+                        scale_to[c] = kv_row_offset(sg, b, hk, P + j, bad_block);
+                    }
+                }
             } else if (err_flag && ch == 0 && blockIdx.x == 0 && hk == 0) {
                 atomicOr(err_flag, SPECVLM_ERR_BAD_BLOCK);
             }
@@ -373,8 +399,12 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_kernel(
     }
     __syncthreads();
 #pragma unroll
-    for (int c = 0; c < kCompactChunksPerThread; ++c)
+    for (int c = 0; c < kCompactChunksPerThread; ++c) {
         if (dst_off[c] >= 0) *reinterpret_cast<uint4*>(base + dst_off[c]) = regs[c];
+        if constexpr (QUANTISED) {
+            if (scale_to[c] >= 0) s_base[scale_to[c]] = static_cast<unsigned char>(scale_of[c]);
+        }
+    }
 }
 
 __global__ void kv_compact_finish_kernel(int B, const int32_t* __restrict__ prefix_len,
@@ -395,22 +425,25 @@ __global__ void kv_compact_finish_kernel(int B, const int32_t* __restrict__ pref
 
 int32_t launch_kv_compact(const specvlm_attn_desc& d, int32_t L, void* k_base, void* v_base,
                           int64_t layer_stride, void* const* k_ptrs, void* const* v_ptrs,
-                          const int32_t* block_table, const int32_t* prefix_len, const int32_t* path,
+                          const specvlm_kv_scales* scales, int64_t scale_layer_stride, void* const* ks_ptrs,
+                          void* const* vs_ptrs, const int32_t* block_table, const int32_t* prefix_len, const int32_t* path,
                           int32_t path_cap, const int32_t* accept_len, int32_t* new_prefix_len,
                           int32_t* moved_idx, int32_t* err_flag, hipStream_t stream) {
-    const int eb = d.dtype == SPECVLM_BF16 ? 2 : 4;
+    const int eb = scales ? 1 : d.dtype == SPECVLM_BF16 ? 2 : 4;
     KvGeom g{d.kv_stride_b, d.kv_stride_h, d.kv_stride_t, d.paged ? block_table : nullptr,
              d.max_blocks_per_req, d.num_blocks,
              d.paged ? d.max_blocks_per_req * SPECVLM_PAGE_SIZE : d.kv_capacity};
-    const int chunk_bits = __builtin_ctz(d.D * eb / 16);           // (8, 16 or 32 chunks of a row)
+    CompactScales cs{};
+    if (scales) cs = CompactScales{scales->k_dev, scales->v_dev, scale_layer_stride, scales->stride_b, scales->stride_h, ks_ptrs, vs_ptrs};
+    const int chunk_bits = __builtin_ctz(d.D * eb / 16);           // (4, 8, 16 or 32 chunks of a row)
     const int head_bits = compact_head_bits(static_cast<int64_t>(L) * 2 * d.B * d.H_kv, path_cap << chunk_bits);
     dim3 grid(L * 2, (d.H_kv + (1 << head_bits) - 1) >> head_bits, d.B);
     // One launch when new_prefix_len is a buffer of its own; when it aliases prefix_len it may only
     // be written after every workgroup has read the old lengths: a second, tiny launch.
     const bool alias = new_prefix_len == prefix_len;
-    hipLaunchKernelGGL(kv_compact_kernel, grid, dim3(kCompactThreads), 0, stream, g,
+    hipLaunchKernelGGL(scales ? kv_compact_kernel<true> : kv_compact_kernel<false>, grid, dim3(kCompactThreads), 0, stream, g,
                        static_cast<unsigned char*>(k_base), static_cast<unsigned char*>(v_base),
-                       layer_stride * eb, k_ptrs, v_ptrs, eb, chunk_bits, head_bits, d.H_kv, prefix_len, path,
+                       layer_stride * eb, k_ptrs, v_ptrs, cs, eb, chunk_bits, head_bits, d.H_kv, prefix_len, path,
                        path_cap, accept_len, alias ? nullptr : new_prefix_len, alias ? nullptr : moved_idx, err_flag);
     int32_t rc = check_launch();
     if (rc || !alias) return rc;

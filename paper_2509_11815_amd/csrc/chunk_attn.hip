@@ -11,12 +11,18 @@
 
 #include "attn_common.hpp"
 #include "attn_rows.hpp"
+#include "wave_ops.hpp"
 
 namespace specvlm {
 
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kLeastRounds = 2;              // rounds a range of keys has at least: below that the meeting of the partial results costs more
+constexpr int kMostColumns = 64;             // ranges of keys of one (request, KV head, row block)
+constexpr int kMostPairs = 1024;             // (request, KV head, row block)s of a call whose keys are divided: more fill the chip by themselves
+constexpr size_t kChunkCounterBytes = kMostPairs * kCounterStride * 4;     // tickets: a 128-byte line each
 
 struct ChunkParams {
     KvGeom g;                                // strides in elements of the cache
@@ -31,7 +37,115 @@ struct ChunkParams {
     int B, N_max, H_q, H_kv, group, row_blocks;
     uint32_t magic_group;
     float scale, c2, tau;                    // softmax scale; times log2 e; how far a score may lie above the reference
+    int target;                              // workgroups to divide the keys among, 0: one range of keys for every (request, KV head, row block)
+    int32_t* ws_cnt;                         // [pairs] arrival tickets, kCounterStride words apart, zero between calls
+    unsigned char* ws_part;                  // [items] partial results, see merge_ranges()
 };
+
+// A workgroup's part of the call: column x of the c ranges of keys of (request, KV head, row block).
+struct Item { int b, hk, rb, x, c, n, P, index; };
+
+__device__ __forceinline__ int wave_sum_int(int x) {
+    x = row_sum(x);
+    return (__builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16)) + (__builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48));
+}
+
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int x, int lane) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);           // row_shr:1, zero where there is none
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    const int a = __builtin_amdgcn_readlane(x, 15), b = a + __builtin_amdgcn_readlane(x, 31), c = b + __builtin_amdgcn_readlane(x, 47);
+    return x + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
+}
+
+// What a workgroup has to do, worked out by each from the lengths, which the host does not know.  Every range of keys of every (request, KV
+// head, row block) gets about the same number of rounds (a round: a tile of every wavefront): the least `len` for which the ranges are no
+// more than `target` workgroups (or one each).  Returns false where there is nothing to do.
+template <int ROWS>
+__device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& it) {
+    typedef const __attribute__((address_space(4))) int32_t* const_i32;
+    auto error_of = [&](int n, int P) { return n < 0 || n > p.N_max ? SPECVLM_ERR_BAD_NUM_NODES : P < 0 || P > p.g.capacity - n ? SPECVLM_ERR_BAD_LENGTH : 0; };
+    if (!p.target) {
+        const uint32_t pair = blockIdx.x / static_cast<uint32_t>(p.row_blocks);
+        it.rb = blockIdx.x - pair * p.row_blocks;
+        it.b = pair / static_cast<uint32_t>(p.H_kv);
+        it.hk = pair - it.b * p.H_kv;
+        it.n = p.num_new ? ((const_i32)p.num_new)[it.b] : p.N_max;
+        it.P = ((const_i32)p.prefix_len)[it.b];
+        it.x = 0;
+        it.c = 1;
+        it.index = blockIdx.x;
+        if (const int err = error_of(it.n, it.P)) {
+            if (it.rb == 0 && it.hk == 0 && threadIdx.x == 0 && p.err_flag) atomicOr(p.err_flag, err);
+            return false;
+        }
+        return it.rb * ROWS < p.group * it.n;
+    }
+    int n = 0, P = 0, rounds = 0, units = 0;               // of request b0 + lane
+    auto look = [&](int b0, bool report) __attribute__((always_inline)) {
+        const int b = b0 + lane;
+        rounds = units = 0;
+        if (b < p.B) {
+            n = p.num_new ? p.num_new[b] : p.N_max;
+            P = p.prefix_len[b];
+            if (const int err = error_of(n, P)) {
+                if (report && p.err_flag) atomicOr(p.err_flag, err);
+            } else if (n) {
+                rounds = static_cast<int>((static_cast<uint32_t>(P + n - 1) + kSharesRound) / kSharesRound);
+                units = (p.group * n + ROWS - 1) / ROWS * p.H_kv;
+            }
+        }
+    };
+    // (more than 64 requests: looked at 64 at a time, again for every pass)
+    const bool first = blockIdx.x == 0 && threadIdx.x < 64;
+    float total = 0.f;
+    int pairs = 0, longest = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        look(b0, first);
+        total += wave_sum(static_cast<float>(rounds) * units);
+        pairs += wave_sum_int(units);
+        longest = max(longest, static_cast<int>(wave_max(static_cast<float>(rounds))));      // (up to 2^24: exact)
+    }
+    const int most = max(p.target, pairs);
+    int len = max(static_cast<int>(ceilf(total / p.target)), max(kLeastRounds, (longest + kMostColumns - 1) / kMostColumns));
+    int all;
+    for (;; len += 1 + (len >> 4)) {
+        all = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            if (p.B > 64) look(b0, false);
+            all += wave_sum_int(units * ((rounds + len - 1) / len));
+        }
+        if (all <= most || len >= longest) break;
+    }
+    // every XCD has a contiguous range of the items, so that the row blocks of a head's keys share an L2
+    const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, share = all >> 3, more = all & 7;
+    if (place >= share + (xcd < more)) return false;
+    it.index = xcd * share + min(xcd, more) + place;
+    int before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        if (p.B > 64) look(b0, false);
+        const int mine = units * ((rounds + len - 1) / len), upto = before + wave_scan(mine, lane);
+        const unsigned long long here = __ballot(it.index < upto);
+        if (here) {
+            const int at = __builtin_ctzll(here);
+            it.b = b0 + at;
+            it.n = __builtin_amdgcn_readlane(n, at);
+            it.P = __builtin_amdgcn_readlane(P, at);
+            const uint32_t local = it.index - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
+            const uint32_t units_of = __builtin_amdgcn_readlane(units, at), blocks = units_of / static_cast<uint32_t>(p.H_kv);
+            it.c = (__builtin_amdgcn_readlane(rounds, at) + len - 1) / len;
+            it.x = local / units_of;
+            const uint32_t rest = local - it.x * units_of;
+            it.hk = rest / blocks;
+            it.rb = rest - it.hk * blocks;
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
 
 __device__ __forceinline__ float max16(const f32x16& a) {
     auto max3 = [](float x, float y, float z) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z); };
@@ -50,6 +164,113 @@ __device__ __forceinline__ float other_half(float x) {
 // LDS traffic between lanes of one wavefront needs no wait (it is in order) but must stay in order.
 __device__ __forceinline__ void wave_order() { asm volatile("" ::: "memory"); }
 
+// Items between two ranges of keys of one (request, KV head, row block): find_item() puts the request's (head, block) pairs in between.
+__device__ __forceinline__ int step_of(const ChunkParams& p, const Item& it, int rows) { return (p.group * it.n + rows - 1) / rows * p.H_kv; }
+
+// The partial results of an item's ranges of keys, in their order, by the 256 threads of the workgroup that came last.  A unit is four head
+// dims of a row; where the block has few rows, threads share a unit's ranges and meet in LDS.
+template <int D, int ROWS>
+__device__ __forceinline__ void merge_ranges(const ChunkParams& p, const Item& it, const unsigned char* parts, int64_t part_step, unsigned char* lds) {
+    constexpr int kCoherent = 16;                          // device-coherent (sc1) loads, which the compiler counts
+    constexpr int NT = D / 32;
+    const int tid = threadIdx.x, row0 = it.rb * ROWS;
+    const int rows = min(ROWS, p.group * it.n - row0);
+    float* const s_w = reinterpret_cast<float*>(lds);      // [rows][c] maxima, then weights
+    float* const s_inv = s_w + ROWS * kMostColumns;        // [rows]
+    float* const s_sum = s_inv + ROWS;                     // [256][4]
+    auto load = [&](int64_t off, auto wide) __attribute__((always_inline)) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(parts), 0, 0x7FFFFFFF, 0x00027000);
+        if constexpr (decltype(wide)::value) return __builtin_amdgcn_raw_buffer_load_b128(rsrc, static_cast<int>(off), 0, kCoherent);
+        else return __builtin_amdgcn_raw_buffer_load_b64(rsrc, static_cast<int>(off), 0, kCoherent);
+    };
+    // eight threads a row: its maximum over the ranges, their weights, the sum
+    for (int r = tid >> 3; r < rows; r += 32) {
+        const int i0 = tid & 7;
+        float m[kMostColumns / 8], l[kMostColumns / 8], M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int k = 0; k < kMostColumns / 8; ++k) {
+            m[k] = -INFINITY;
+            l[k] = 0.f;
+            if (i0 + 8 * k < it.c) {
+                const u32x2 ml = load((i0 + 8 * k) * part_step + ROWS * D * 4 + r * 8, std::false_type{});
+                m[k] = __uint_as_float(ml[0]);
+                l[k] = __uint_as_float(ml[1]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kMostColumns / 8; ++k) M = __builtin_elementwise_maximum(M, m[k]);
+        M = __builtin_elementwise_maximum(M, dpp<0x141>(M));
+        M = __builtin_elementwise_maximum(M, dpp<0x4E>(M));
+        M = __builtin_elementwise_maximum(M, dpp<0xB1>(M));
+        const float m_safe = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int k = 0; k < kMostColumns / 8; ++k) {
+            const float w = fast_exp2((m[k] - m_safe) * p.c2);
+            L += l[k] * w;
+            if (i0 + 8 * k < it.c) s_w[r * kMostColumns + i0 + 8 * k] = w;
+        }
+        L += dpp<0x141>(L);
+        L += dpp<0x4E>(L);
+        L += dpp<0xB1>(L);
+        if (i0 == 0) {
+            s_inv[r] = 1.f / L;
+            if (p.lse) {
+                const int token = divide(row0 + r, p.magic_group);
+                const int h = it.hk * p.group + row0 + r - token * p.group;
+                p.lse[(static_cast<int64_t>(it.b) * p.H_q + h) * p.N_max + token] = M * p.scale + __log2f(L) * kLn2;
+            }
+        }
+    }
+    __syncthreads();
+    // Units of 32 rows at a time: (dims 32t + 8u + 4hf .., row), rows innermost, so that threads beside one another read beside one another.
+    for (int q = 0; q < ROWS; q += 32) {
+        const int here = min(32, rows - q);
+        if (here <= 0) break;
+        const int units = here * (D / 4);
+        int share = 1;                                     // threads of a unit
+        while (units * share * 2 <= 256) share *= 2;
+        for (int first = 0; first < units; first += 256 / share) {
+            const int part = tid * share / 256;            // (share is a power of two)
+            const int unit = first + tid - part * (256 / share);
+            const bool mine = unit < units;
+            const int dims = mine ? unit / here : 0, r = mine ? unit - dims * here : 0;
+            const int hf = dims & 1, block = q / 32 * NT + (dims >> 3), u = (dims >> 1) & 3;
+            const int off = ((block * 4 + u) * 64 + hf * 32 + r) * 16;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            constexpr int BATCH = 8;
+            for (int i = part; i < it.c; i += share * BATCH) {
+                u32x4 x[BATCH];
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) x[k] = load(min(i + k * share, it.c - 1) * part_step + off, std::true_type{});
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const float w = i + k * share < it.c ? s_w[(q + r) * kMostColumns + i + k * share] : 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(__uint_as_float(x[k][e]), w, sum[e]);
+                }
+            }
+            if (share > 1) {
+                __syncthreads();
+                reinterpret_cast<f32x4*>(s_sum)[tid] = sum;
+                __syncthreads();
+                if (part == 0)
+                    for (int k = 1; k < share; ++k) {
+                        const f32x4 other = reinterpret_cast<const f32x4*>(s_sum)[tid + k * (256 / share)];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[e] += other[e];
+                    }
+            }
+            if (mine && part == 0) {
+                const float inv = s_inv[q + r];
+                const int token = divide(row0 + q + r, p.magic_group);
+                const int h = it.hk * p.group + row0 + q + r - token * p.group;
+                uint16_t* const to = p.o + it.b * p.o_sb + token * p.o_sn + h * p.o_sh + dims * 4;
+                *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(sum[0] * inv, sum[1] * inv), pack_bf16x2(sum[2] * inv, sum[3] * inv)};
+            }
+        }
+    }
+}
+
 template <int D, int QB, bool E4M3, bool PAGED>
 __device__ __forceinline__ void attend(const ChunkParams& p) {
     constexpr int NC = D / 16;                 // contraction steps of K Q^T
@@ -61,6 +282,7 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
     constexpr int KI = kKeys / RPI;            // load instructions per tile
     constexpr int kTileBytes = kKeys * ROWB;
     constexpr int ROWS = QB * 32;
+    constexpr bool LEAN = QB == 1;             // little in registers, so that two workgroups fit a compute unit
     constexpr int NB = QB * NT;                // (32 rows, 32 dims) blocks of the result
     constexpr int OWN = NB >= kWaveWgs ? NB / kWaveWgs : 1;
     constexpr int kMergeBytes = NB * 3 * 4096;
@@ -70,28 +292,13 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
     __shared__ float s_m[kWaveWgs][ROWS];
     __shared__ float s_l[kWaveWgs][ROWS];
 
-    const uint32_t pair = blockIdx.x / static_cast<uint32_t>(p.row_blocks);
-    const int rb = blockIdx.x - pair * p.row_blocks;
-    const int b = pair / static_cast<uint32_t>(p.H_kv);
-    const int hk = pair - b * p.H_kv;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, hf = lane >> 5;
-
-    typedef const __attribute__((address_space(4))) int32_t* const_i32;
-    const int n = p.num_new ? ((const_i32)p.num_new)[b] : p.N_max;
-    const int P = ((const_i32)p.prefix_len)[b];
-    int err = 0;
-    if (n < 0 || n > p.N_max) err |= SPECVLM_ERR_BAD_NUM_NODES;
-    else if (P < 0 || P > p.g.capacity - n) err |= SPECVLM_ERR_BAD_LENGTH;
-    const bool reports = rb == 0 && hk == 0 && tid == 0 && p.err_flag;
-    if (err) {
-        if (reports) atomicOr(p.err_flag, err);
-        return;
-    }
-    const int row0 = rb * ROWS;
-    if (row0 >= p.group * n) return;
-    const int S = P + n;
+    Item it;
+    if (!find_item<ROWS>(p, lane, it)) return;
+    const int b = it.b, hk = it.hk, n = it.n, P = it.P, S = P + n;
+    const int row0 = it.rb * ROWS;
 
     // Rows of this lane: token and head of the group.
     int token[QB], head[QB];
@@ -113,7 +320,7 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
         int par = lane < n ? p.parent[static_cast<int64_t>(b) * p.N_max + lane] : -1;
         const bool bad_par = lane < n && (lane == 0 ? par != -1 : (par < 0 || par >= lane));
         if (__any(bad_par)) {                              // the same in every workgroup of the request
-            if (reports) atomicOr(p.err_flag, SPECVLM_ERR_BAD_PARENT);
+            if (it.rb == 0 && it.hk == 0 && it.x == 0 && tid == 0 && p.err_flag) atomicOr(p.err_flag, SPECVLM_ERR_BAD_PARENT);
             return;
         }
         uint32_t mlo = lane < 32 ? 1u << (lane & 31) : 0u, mhi = lane < 32 ? 0u : 1u << (lane & 31);
@@ -133,8 +340,12 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
     }
     const int all_see = p.parent ? P : P + first_token + 1;          // slots that every row of the block sees
     const int end = p.parent ? S : P + last_token + 1;               // slots that some row sees
-    const int ntile = (end + kKeys - 1) / kKeys;
-    const int my_tiles = wave < ntile ? (ntile - wave + kWaveWgs - 1) / kWaveWgs : 0;
+    // Tiles of this range of keys: whole rounds of the request, up to the block's end; this wavefront's stream has every fourth.
+    const int rounds = static_cast<int>((static_cast<uint32_t>(S - 1) + kSharesRound) / kSharesRound);
+    const int first_round = it.x * rounds / it.c, next_round = (it.x + 1) * rounds / it.c;
+    const int ntile = min((end - 1) / kKeys + 1, next_round * kWaveWgs);
+    const int tile0 = first_round * kWaveWgs + wave;
+    const int my_tiles = tile0 < ntile ? (ntile - tile0 + kWaveWgs - 1) / kWaveWgs : 0;
 
     // ---- tile fetch -------------------------------------------------------------------------
     const int lrow = lane / LPR, lpos = lane % LPR;
@@ -147,7 +358,7 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
     // Block ids: lane 2i + x holds that of half x of tile i (mod 32) of the stream, and the next 32 tiles' are on their way
     int ids = 0, ids_next = 0;
     auto request_ids = [&](int j) __attribute__((always_inline)) {
-        const int blk = min((wave + (j + (lane >> 1)) * kWaveWgs) * 2 + (lane & 1), last_blk);
+        const int blk = min((tile0 + (j + (lane >> 1)) * kWaveWgs) * 2 + (lane & 1), last_blk);
         return p.g.block_table[static_cast<int64_t>(b) * p.g.max_blocks + blk];
     };
     auto take_ids = [&](int raw) __attribute__((always_inline)) {
@@ -156,7 +367,7 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
     };
     struct Raw { u32x4 w[KI]; uint32_t e[E4M3 ? KI : 1]; };
     auto load = [&](Raw& raw, const unsigned char* cache, const unsigned char* scales, int j) __attribute__((always_inline)) {
-        const int slot0 = (wave + j * kWaveWgs) * kKeys;
+        const int slot0 = (tile0 + j * kWaveWgs) * kKeys;
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
             const unsigned char *base, *sbase = scales + s_off;
@@ -284,26 +495,25 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
             load(vraw, p.v, p.vs, 1);
         }
         wave_order();
-        read_k();
-#pragma unroll
-        for (int t = 0; t < NT; ++t) read_v(t);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) scores(s[qb], qb);
-        wave_order();
-        if (my_tiles > 1) {
-            store(kraw, std::false_type{});
-            wave_order();
+        if constexpr (!LEAN) {
             read_k();
-            if (my_tiles > 2) load(kraw, p.k, p.ks, 2);
-        }
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) lmax[qb] = max16(s[qb]);
+            for (int t = 0; t < NT; ++t) read_v(t);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) scores(s[qb], qb);
+            wave_order();
+            if (my_tiles > 1) {
+                store(kraw, std::false_type{});
+                wave_order();
+                read_k();
+                if (my_tiles > 2) load(kraw, p.k, p.ks, 2);
+            }
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) lmax[qb] = max16(s[qb]);
+        }
     }
-    // One tile.  At its start s holds its scores and lmax their maxima; va its V operands, ka the next tile's K operands; vraw and kraw V of the
-    // next tile and K of the one after it.
-    auto step = [&](auto next, int j) __attribute__((always_inline)) {
-        constexpr bool NEXT = decltype(next)::value;
-        const int slot0 = (wave + j * kWaveWgs) * kKeys;
+    // Masks and reference maxima of the tile of slot0, whose scores s and their maxima lmax are.
+    auto settle = [&](int slot0) __attribute__((always_inline)) {
         if (slot0 + kKeys > all_see) {
             // bit k of `visible`: key slot0 + k.  Its place among this lane's scores is a constant once the lane's half is shifted out
 #pragma unroll
@@ -343,6 +553,12 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
                 for (int t = 0; t < NT; ++t) acc[qb][t] *= alpha;
             }
         }
+    };
+    // One tile.  At its start s holds its scores and lmax their maxima; va its V operands, ka the next tile's K operands; vraw and kraw V of the
+    // next tile and K of the one after it.
+    auto step = [&](auto next, int j) __attribute__((always_inline)) {
+        constexpr bool NEXT = decltype(next)::value;
+        settle((tile0 + j * kWaveWgs) * kKeys);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             if constexpr (NEXT) scores(s_next[qb], qb);
@@ -381,7 +597,40 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
             for (int qb = 0; qb < QB; ++qb) { s[qb] = s_next[qb]; lmax[qb] = max16(s[qb]); }
         }
     };
-    {
+    // The same without anything of the next tile in registers but what has been loaded of it: two workgroups fit a compute unit.
+    auto lean_step = [&](int j) __attribute__((always_inline)) {
+        read_k();
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) { scores(s[qb], qb); lmax[qb] = max16(s[qb]); }
+        settle((tile0 + j * kWaveWgs) * kKeys);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) weights(qb);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            read_v(t);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) acc[qb][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[t][x], pf[qb][x], acc[qb][t], 0, 0, 0);
+        }
+        wave_order();
+        if (j + 1 < my_tiles) {
+            store(kraw, std::false_type{});
+            store(vraw, std::true_type{});
+            if (j + 2 < my_tiles) {
+                if (PAGED && ((j + 2) & 31) == 0) {
+                    take_ids(ids_next);
+                    if (j + 2 + 32 < my_tiles) ids_next = request_ids(j + 2 + 32);
+                }
+                load(kraw, p.k, p.ks, j + 2);
+                load(vraw, p.v, p.vs, j + 2);
+            }
+            wave_order();
+        }
+    };
+    if constexpr (LEAN) {
+        for (int j = 0; j < my_tiles; ++j) lean_step(j);
+    } else {
         int j = 0;
         for (; j < my_tiles - 1; ++j) step(std::true_type{}, j);
         if (my_tiles > 0) step(std::false_type{}, j);
@@ -417,54 +666,102 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
         }
     }
     __syncthreads();
-    if (wave >= NB / OWN) return;
+    float M[OWN], L[OWN];
+    if (wave < NB / OWN) {
 #pragma unroll
-    for (int e = 0; e < OWN; ++e) {
-        const int block = wave * OWN + e;
-        const int qb = block / NT, t = block % NT;
-        float m[kWaveWgs], w[kWaveWgs];
+        for (int e = 0; e < OWN; ++e) {
+            const int block = wave * OWN + e;
+            const int qb = block / NT;
+            float m[kWaveWgs], w[kWaveWgs];
 #pragma unroll
-        for (int x = 0; x < kWaveWgs; ++x) m[x] = s_m[x][qb * 32 + l32];
-        const float M = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-        const float m_safe = M == -INFINITY ? 0.f : M;
-        float L = 0.f;
+            for (int x = 0; x < kWaveWgs; ++x) m[x] = s_m[x][qb * 32 + l32];
+            M[e] = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            const float m_safe = M[e] == -INFINITY ? 0.f : M[e];
+            L[e] = 0.f;
 #pragma unroll
-        for (int x = 0; x < kWaveWgs; ++x) {               // (in this order in every owner of the rows)
-            w[x] = fast_exp2((m[x] - m_safe) * p.c2);
-            L += s_l[x][qb * 32 + l32] * w[x];
-        }
-        out[e] *= wave == 0 ? w[0] : wave == 1 ? w[1] : wave == 2 ? w[2] : w[3];
-        const f32x4* src = reinterpret_cast<const f32x4*>(s_mem) + block * 3 * 4 * 64 + lane;
+            for (int x = 0; x < kWaveWgs; ++x) {           // (in this order in every owner of the rows)
+                w[x] = fast_exp2((m[x] - m_safe) * p.c2);
+                L[e] += s_l[x][qb * 32 + l32] * w[x];
+            }
+            out[e] *= wave == 0 ? w[0] : wave == 1 ? w[1] : wave == 2 ? w[2] : w[3];
+            const f32x4* src = reinterpret_cast<const f32x4*>(s_mem) + block * 3 * 4 * 64 + lane;
 #pragma unroll
-        for (int idx = 0; idx < 3; ++idx) {
-            const float wx = wave <= idx ? w[idx + 1] : w[idx];
+            for (int idx = 0; idx < 3; ++idx) {
+                const float wx = wave <= idx ? w[idx + 1] : w[idx];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const f32x4 v = src[(idx * 4 + u) * 64];
+                for (int u = 0; u < 4; ++u) {
+                    const f32x4 v = src[(idx * 4 + u) * 64];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) out[e][4 * u + i] += v[i] * wx;
+                    for (int i = 0; i < 4; ++i) out[e][4 * u + i] += v[i] * wx;
+                }
             }
         }
-        const bool live = QB == 1 ? real[0] : qb ? real[QB - 1] : real[0];
-        const int tok = QB == 1 ? token[0] : qb ? token[QB - 1] : token[0], h = QB == 1 ? head[0] : qb ? head[QB - 1] : head[0];
-        const float inv = 1.f / L;
-        uint16_t* const row = p.o + b * p.o_sb + tok * p.o_sn + h * p.o_sh + 32 * t + 8 * hf;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {                      // 16 dims: registers 8u .. 8u + 7
-            uint32_t x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = pack_bf16x2(out[e][8 * u + 2 * i] * inv, out[e][8 * u + 2 * i + 1] * inv);
-            // the halves of the wavefront hold dims 0-3, 8-11 and 4-7, 12-15: the lower keeps 0-7, the upper 8-15
-            const auto r0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
-            const auto r1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
-            if (live) *reinterpret_cast<u32x4*>(row + 16 * u) = u32x4{r0[0], r1[0], r0[1], r1[1]};
-        }
-        if (live && p.lse && hf == 0 && t == 0) p.lse[(static_cast<int64_t>(b) * p.H_q + h) * p.N_max + tok] = M * p.scale + __log2f(L) * kLn2;
     }
+    if (it.c == 1) {
+        if (wave < NB / OWN) {
+#pragma unroll
+            for (int e = 0; e < OWN; ++e) {
+                const int block = wave * OWN + e, qb = block / NT, t = block % NT;
+                const bool live = qb ? real[QB - 1] : real[0];
+                const int tok = qb ? token[QB - 1] : token[0], h = qb ? head[QB - 1] : head[0];
+                const float inv = 1.f / L[e];
+                uint16_t* const row = p.o + b * p.o_sb + tok * p.o_sn + h * p.o_sh + 32 * t + 8 * hf;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {              // 16 dims: registers 8u .. 8u + 7
+                    uint32_t x[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = pack_bf16x2(out[e][8 * u + 2 * i] * inv, out[e][8 * u + 2 * i + 1] * inv);
+                    // the halves of the wavefront hold dims 0-3, 8-11 and 4-7, 12-15: the lower keeps 0-7, the upper 8-15
+                    const auto r0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
+                    const auto r1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+                    if (live) *reinterpret_cast<u32x4*>(row + 16 * u) = u32x4{r0[0], r1[0], r0[1], r1[1]};
+                }
+                if (live && p.lse && hf == 0 && t == 0) p.lse[(static_cast<int64_t>(b) * p.H_q + h) * p.N_max + tok] = M[e] * p.scale + __log2f(L[e]) * kLn2;
+            }
+        }
+        return;
+    }
+    // ---- partial result of this range of keys, and the merge by the last of them -----------------
+    // A partial: [block][4][64 lanes] vectors of four fp32 (the accumulators as they are, rows of the group that exist only), then a (maximum,
+    // sum) pair per row.
+    constexpr int kPartBytes = ROWS * (D + 2) * 4;
+    unsigned char* const parts = p.ws_part + static_cast<int64_t>(it.index - it.x * step_of(p, it, ROWS)) * kPartBytes;
+    const int64_t part_step = static_cast<int64_t>(step_of(p, it, ROWS)) * kPartBytes;
+    if (wave < NB / OWN) {
+        unsigned char* const mine = parts + it.x * part_step;
+#pragma unroll
+        for (int e = 0; e < OWN; ++e) {
+            const int block = wave * OWN + e, qb = block / NT;
+            if (!(qb ? real[QB - 1] : real[0])) continue;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                u32x4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(out[e][4 * u + i]);
+                store16_coherent(mine + ((block * 4 + u) * 64 + lane) * 16, x);
+            }
+            if (block % NT == 0 && hf == 0)
+                store8_coherent(mine + ROWS * D * 4 + (qb * 32 + l32) * 8, u32x2{__float_as_uint(M[e]), __float_as_uint(L[e])});
+        }
+    }
+    wait_vmcnt<0>();
+    __syncthreads();                                       // (LDS is free as well)
+    int* const s_last = reinterpret_cast<int*>(s_m);
+    if (tid == 0) {
+        int32_t* const cnt = p.ws_cnt + ((static_cast<int64_t>(b) * p.H_kv + hk) * p.row_blocks + it.rb) * kCounterStride;
+        const int ticket = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const bool last = ticket == it.c - 1;
+        if (last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *s_last = last;
+    }
+    __syncthreads();
+    if (!*s_last) return;
+    asm volatile("" ::: "memory");
+    merge_ranges<D, ROWS>(p, it, parts, part_step, s_mem);
 }
 
 template <int D, int QB, bool E4M3, bool PAGED>
-__global__ __launch_bounds__(kWaveWgs * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void chunk_attn_kernel(ChunkParams p) {
+__global__ __launch_bounds__(kWaveWgs * 64) __attribute__((amdgpu_waves_per_eu(QB == 1 ? 2 : 1, QB == 1 ? 2 : 1))) void chunk_attn_kernel(ChunkParams p) {
     attend<D, QB, E4M3, PAGED>(p);
 }
 
@@ -475,13 +772,46 @@ void launch_as(const ChunkParams& p, bool e4m3, dim3 grid, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, grid, dim3(kWaveWgs * 64), 0, stream, p);
 }
 
+
+struct ChunkPlan {
+    int qb;                  // blocks of 32 rows per workgroup
+    int row_blocks, target;  // see ChunkParams
+    int64_t workgroups;
+    size_t bytes;            // workspace
+};
+
+// How a call is divided, with `bytes` of workspace.
+ChunkPlan chunk_plan(const specvlm_attn_desc& d, size_t bytes) {
+    ChunkPlan plan;
+    const int64_t rows = static_cast<int64_t>(d.H_q / d.H_kv) * d.N_max;
+    plan.qb = rows <= 32 ? 1 : 2;
+    plan.row_blocks = static_cast<int>((rows + 32 * plan.qb - 1) / (32 * plan.qb));
+    const int64_t pairs = static_cast<int64_t>(d.B) * d.H_kv * plan.row_blocks;
+    plan.target = 0;
+    plan.workgroups = pairs;
+    plan.bytes = 0;
+    const int64_t capacity = d.paged ? static_cast<int64_t>(d.max_blocks_per_req) * SPECVLM_PAGE_SIZE : d.kv_capacity;
+    const int64_t rounds = (capacity + kSharesRound - 1) / kSharesRound;
+    if (d.num_splits == 1 || pairs > kMostPairs || rounds <= kLeastRounds || bytes < kChunkCounterBytes) return plan;
+    const int64_t part = static_cast<int64_t>(32) * plan.qb * (d.D + 2) * 4;
+    const int64_t slots = (bytes - kChunkCounterBytes) / part;
+    const int64_t want = std::max<int64_t>(plan.qb == 1 ? 512 : 256, pairs);
+    const int64_t most = std::min(want, pairs * std::min<int64_t>(kMostColumns, (rounds + kLeastRounds - 1) / kLeastRounds));
+    if (slots < pairs) return plan;
+    plan.target = static_cast<int>(std::min(most, slots));
+    plan.workgroups = (plan.target + 7) / 8 * 8;
+    plan.bytes = kChunkCounterBytes + plan.target * part;
+    return plan;
+}
+
 }  // namespace
 
-size_t chunk_workspace_bytes(const specvlm_attn_desc&) { return 0; }
+size_t chunk_workspace_bytes(const specvlm_attn_desc& d) { return chunk_plan(d, SPECVLM_CHUNK_WORKSPACE_BYTES).bytes; }
 
 int32_t launch_chunk_attn(const ChunkArgs& a) {
     const specvlm_attn_desc& d = a.d;
-    constexpr int kRows = 64;
+    const ChunkPlan plan = chunk_plan(d, a.workspace_bytes);
+    if (plan.workgroups >= int64_t{1} << 31) return SPECVLM_INVALID_ARG;
     ChunkParams p;
     p.g = KvGeom{d.kv_stride_b, d.kv_stride_h, d.kv_stride_t, d.paged ? a.block_table : nullptr, d.max_blocks_per_req, d.num_blocks,
                  d.paged ? d.max_blocks_per_req * SPECVLM_PAGE_SIZE : d.kv_capacity};
@@ -493,16 +823,17 @@ int32_t launch_chunk_attn(const ChunkArgs& a) {
     p.o_sb = d.o_stride_b; p.o_sn = d.o_stride_n; p.o_sh = d.o_stride_h;
     p.prefix_len = a.prefix_len; p.num_new = a.num_new; p.parent = a.parent; p.err_flag = a.err_flag;
     p.B = d.B; p.N_max = d.N_max; p.H_q = d.H_q; p.H_kv = d.H_kv; p.group = d.H_q / d.H_kv;
-    p.row_blocks = (p.group * d.N_max + kRows - 1) / kRows;
+    p.row_blocks = plan.row_blocks;
     p.magic_group = divisor(p.group);
     p.scale = a.scale;
     p.c2 = a.scale * kLog2e;
     p.tau = std::fmin(kTau / p.c2, 1e30f);
-    const int64_t workgroups = static_cast<int64_t>(d.B) * d.H_kv * p.row_blocks;
-    if (workgroups >= int64_t{1} << 31) return SPECVLM_INVALID_ARG;
-    const dim3 grid(static_cast<unsigned>(workgroups));
-    if (d.D == 128) launch_as<128, 2>(p, a.scales != nullptr, grid, a.stream);
-    else launch_as<64, 2>(p, a.scales != nullptr, grid, a.stream);
+    p.target = plan.target;
+    p.ws_cnt = static_cast<int32_t*>(a.workspace);
+    p.ws_part = static_cast<unsigned char*>(a.workspace) + kChunkCounterBytes;
+    const dim3 grid(static_cast<unsigned>(plan.workgroups));
+    if (d.D == 128) plan.qb == 1 ? launch_as<128, 1>(p, a.scales != nullptr, grid, a.stream) : launch_as<128, 2>(p, a.scales != nullptr, grid, a.stream);
+    else plan.qb == 1 ? launch_as<64, 1>(p, a.scales != nullptr, grid, a.stream) : launch_as<64, 2>(p, a.scales != nullptr, grid, a.stream);
     return check_launch();
 }
 

@@ -19,6 +19,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr int kSharedRows = 256;             // rows of a workgroup whose wavefronts share tiles
 constexpr int kLeastRounds = 2;              // rounds a range of keys has at least: below that the meeting of the partial results costs more
 constexpr int kMostColumns = 64;             // ranges of keys of one (request, KV head, row block)
 constexpr int kMostPairs = 1024;             // (request, KV head, row block)s of a call whose keys are divided: more fill the chip by themselves
@@ -60,13 +61,30 @@ __device__ __forceinline__ int wave_scan(int x, int lane) {
     return x + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
 }
 
+__device__ __forceinline__ int length_error(const ChunkParams& p, int n, int P) {
+    return n < 0 || n > p.N_max ? SPECVLM_ERR_BAD_NUM_NODES : P < 0 || P > p.g.capacity - n ? SPECVLM_ERR_BAD_LENGTH : 0;
+}
+
+// A 32 x 32 block of O^T (dims 8 (i / 4) + 4 (lane / 32) + i % 4 of the lane's row) times inv, as bf16; `to`: the row's dims 8 (lane / 32) ..
+__device__ __forceinline__ void store_block(const f32x16& a, float inv, uint16_t* to, bool live) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {                          // 16 dims: registers 8u .. 8u + 7
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = pack_bf16x2(a[8 * u + 2 * i] * inv, a[8 * u + 2 * i + 1] * inv);
+        // the halves of the wavefront hold dims 0-3, 8-11 and 4-7, 12-15: the lower keeps 0-7, the upper 8-15
+        const auto r0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
+        const auto r1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+        if (live) *reinterpret_cast<u32x4*>(to + 16 * u) = u32x4{r0[0], r1[0], r0[1], r1[1]};
+    }
+}
+
 // What a workgroup has to do, worked out by each from the lengths, which the host does not know.  Every range of keys of every (request, KV
 // head, row block) gets about the same number of rounds (a round: a tile of every wavefront): the least `len` for which the ranges are no
 // more than `target` workgroups (or one each).  Returns false where there is nothing to do.
 template <int ROWS>
 __device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& it) {
     typedef const __attribute__((address_space(4))) int32_t* const_i32;
-    auto error_of = [&](int n, int P) { return n < 0 || n > p.N_max ? SPECVLM_ERR_BAD_NUM_NODES : P < 0 || P > p.g.capacity - n ? SPECVLM_ERR_BAD_LENGTH : 0; };
     if (!p.target) {
         const uint32_t pair = blockIdx.x / static_cast<uint32_t>(p.row_blocks);
         it.rb = blockIdx.x - pair * p.row_blocks;
@@ -77,7 +95,7 @@ __device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& 
         it.x = 0;
         it.c = 1;
         it.index = blockIdx.x;
-        if (const int err = error_of(it.n, it.P)) {
+        if (const int err = length_error(p, it.n, it.P)) {
             if (it.rb == 0 && it.hk == 0 && threadIdx.x == 0 && p.err_flag) atomicOr(p.err_flag, err);
             return false;
         }
@@ -90,7 +108,7 @@ __device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& 
         if (b < p.B) {
             n = p.num_new ? p.num_new[b] : p.N_max;
             P = p.prefix_len[b];
-            if (const int err = error_of(n, P)) {
+            if (const int err = length_error(p, n, P)) {
                 if (report && p.err_flag) atomicOr(p.err_flag, err);
             } else if (n) {
                 rounds = static_cast<int>((static_cast<uint32_t>(P + n - 1) + kSharesRound) / kSharesRound);
@@ -705,17 +723,7 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
                 const bool live = qb ? real[QB - 1] : real[0];
                 const int tok = qb ? token[QB - 1] : token[0], h = qb ? head[QB - 1] : head[0];
                 const float inv = 1.f / L[e];
-                uint16_t* const row = p.o + b * p.o_sb + tok * p.o_sn + h * p.o_sh + 32 * t + 8 * hf;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {              // 16 dims: registers 8u .. 8u + 7
-                    uint32_t x[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = pack_bf16x2(out[e][8 * u + 2 * i] * inv, out[e][8 * u + 2 * i + 1] * inv);
-                    // the halves of the wavefront hold dims 0-3, 8-11 and 4-7, 12-15: the lower keeps 0-7, the upper 8-15
-                    const auto r0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
-                    const auto r1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
-                    if (live) *reinterpret_cast<u32x4*>(row + 16 * u) = u32x4{r0[0], r1[0], r0[1], r1[1]};
-                }
+                store_block(out[e], inv, p.o + b * p.o_sb + tok * p.o_sn + h * p.o_sh + 32 * t + 8 * hf, live);
                 if (live && p.lse && hf == 0 && t == 0) p.lse[(static_cast<int64_t>(b) * p.H_q + h) * p.N_max + tok] = M[e] * p.scale + __log2f(L[e]) * kLn2;
             }
         }
@@ -760,6 +768,314 @@ __device__ __forceinline__ void attend(const ChunkParams& p) {
     merge_ranges<D, ROWS>(p, it, parts, part_step, s_mem);
 }
 
+// 256 rows a workgroup: every wavefront has 64 rows of its own, and all four share each tile of 32 keys.
+template <int D, bool E4M3, bool PAGED>
+__device__ __forceinline__ void attend_rows(const ChunkParams& p) {
+    constexpr int QB = 2;
+    constexpr int NC = D / 16, NT = D / 32, ROWG = D / 8, ROWB = D * 2;
+    constexpr int LPR = (E4M3 ? D : 2 * D) / 16;   // lanes per cached row
+    constexpr int RPI = 64 / LPR;              // rows per load instruction
+    constexpr int KI = 16 / RPI;               // load instructions of a wavefront per tile: 16 rows of K or of V
+    constexpr int kTileBytes = kKeys * ROWB;
+
+    __shared__ __attribute__((aligned(1024))) unsigned char s_mem[4 * kTileBytes];      // two K tiles, two V tiles
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, hf = lane >> 5;
+    // the blocks with the most keys first; the blocks of a head's keys on one XCD where the number of heads allows it
+    const uint32_t pairs = static_cast<uint32_t>(p.B) * p.H_kv;
+    const uint32_t level = blockIdx.x / pairs, pair = blockIdx.x - level * pairs;
+    const int rb = p.row_blocks - 1 - level;
+    const int b = pair / static_cast<uint32_t>(p.H_kv), hk = pair - b * p.H_kv;
+    typedef const __attribute__((address_space(4))) int32_t* const_i32;
+    const int n = p.num_new ? ((const_i32)p.num_new)[b] : p.N_max;
+    const int P = ((const_i32)p.prefix_len)[b];
+    if (const int err = length_error(p, n, P)) {
+        if (rb == 0 && hk == 0 && tid == 0 && p.err_flag) atomicOr(p.err_flag, err);
+        return;
+    }
+    const int row0 = rb * kSharedRows;
+    if (row0 >= p.group * n) return;
+    const int S = P + n;
+
+    int token[QB], head[QB];
+    bool real[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int R = row0 + wave * 64 + qb * 32 + l32;
+        token[qb] = divide(R, p.magic_group);
+        head[qb] = hk * p.group + R - token[qb] * p.group;
+        real[qb] = token[qb] < n;
+        if (!real[qb]) { token[qb] = n - 1; head[qb] = hk * p.group; }
+    }
+    const int first_token = min(static_cast<int>(divide(row0 + wave * 64, p.magic_group)), n - 1);
+    const int last_token = min(static_cast<int>(divide(row0 + kSharedRows - 1, p.magic_group)), n - 1);
+    const int all_see = P + first_token + 1;   // slots that every row of the wavefront sees
+    const int ntile = (P + last_token) / kKeys + 1;
+
+    // ---- tile fetch: wavefronts 0, 1 bring the halves of K tiles, 2, 3 those of V tiles ---------
+    const bool is_v = wave >> 1;
+    const int half = wave & 1;
+    const int lrow = lane / LPR, lpos = lane % LPR;
+    const int es = E4M3 ? 1 : 2;
+    const uint32_t row_bytes = static_cast<uint32_t>(p.g.stride_t) * es;
+    const unsigned char* const cache = (is_v ? p.v : p.k) + (hk * p.g.stride_h + (PAGED ? 0 : b * p.g.stride_b)) * es;
+    const unsigned char* const scales = (is_v ? p.vs : p.ks) + (hk * p.s_sh + (PAGED ? 0 : b * p.s_sb));
+    const int last_blk = (S - 1) >> 4;
+    bool bad_block = false;
+    int ids = 0, ids_next = 0;                 // lane i: the block of this half of tile i (mod 64), and of the next 64 tiles
+    auto request_ids = [&](int tile) __attribute__((always_inline)) {
+        return p.g.block_table[static_cast<int64_t>(b) * p.g.max_blocks + min((tile + lane) * 2 + half, last_blk)];
+    };
+    auto take_ids = [&](int raw) __attribute__((always_inline)) {
+        bad_block = bad_block || static_cast<uint32_t>(raw) >= static_cast<uint32_t>(p.g.num_blocks);
+        ids = min(max(raw, 0), p.g.num_blocks - 1);
+    };
+    struct Raw { u32x4 w[KI]; uint32_t e[E4M3 ? KI : 1]; };
+    // Tiles are asked for in order, 0, 1, 2 ..; one past the last is not.
+    auto load = [&](Raw& raw, int tile) __attribute__((always_inline)) {
+        if (tile >= ntile) return;
+        const int slot0 = tile * kKeys + half * 16;
+        const unsigned char *base, *sbase;
+        int last;                              // row of the half that is the last to exist (or before it, then some row of the tile again)
+        if constexpr (PAGED) {
+            if (tile && (tile & 63) == 0) {
+                take_ids(ids_next);
+                ids_next = request_ids(tile + 64);
+            }
+            const int blk = __builtin_amdgcn_readlane(ids, tile & 63);
+            base = cache + blk * (p.g.stride_b * es);
+            sbase = scales + blk * p.s_sb;
+            last = (slot0 >> 4) >= last_blk ? (S - 1) & 15 : 15;
+        } else {
+            const int from = min(slot0, (S - 1) & ~15);
+            base = cache + static_cast<int64_t>(from) * row_bytes;
+            sbase = scales + from;
+            last = S - 1 - from;
+        }
+#pragma unroll
+        for (int i = 0; i < KI; ++i) {
+            const uint32_t row = min(i * RPI + lrow, last);
+            raw.w[i] = *reinterpret_cast<const u32x4*>(base + (row * row_bytes + lpos * 16));
+            if constexpr (E4M3) raw.e[i] = sbase[row];
+        }
+    };
+    auto vswz = [](int r) { return D == 128 ? (r & 3) : ((r >> 1) & 1); };
+    uint32_t to[KI][E4M3 ? 2 : 1];             // where this lane's granules go in a tile
+#pragma unroll
+    for (int i = 0; i < KI; ++i) {
+        const int r = half * 16 + i * RPI + lrow;
+        const int swz = is_v ? vswz(r) << 2 : r & (ROWG - 1);
+#pragma unroll
+        for (int h = 0; h < (E4M3 ? 2 : 1); ++h) to[i][h] = (is_v ? 2 * kTileBytes : 0) + r * ROWB + (((E4M3 ? 2 * lpos + h : lpos) ^ swz) << 4);
+    }
+    auto store = [&](const Raw& raw, int slot) __attribute__((always_inline)) {
+        unsigned char* const tile = s_mem + slot * kTileBytes;
+#pragma unroll
+        for (int i = 0; i < KI; ++i) {
+            if constexpr (E4M3) {
+                const float scale = __uint_as_float(raw.e[i] << 23);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x4 w;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        w[2 * x] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw.w[i][2 * h + x], scale, false));
+                        w[2 * x + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw.w[i][2 * h + x], scale, true));
+                    }
+                    *reinterpret_cast<u32x4*>(tile + to[i][h]) = w;
+                }
+            } else {
+                *reinterpret_cast<u32x4*>(tile + to[i][0]) = raw.w[i];
+            }
+        }
+    };
+
+    // ---- operands, as in attend() -----------------------------------------------------------
+    uint32_t kaddr[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kaddr[c] = l32 * ROWB + (((2 * c + hf) ^ (l32 & (ROWG - 1))) << 4);
+    const int k0 = 4 * hf + ((lane & 15) >> 2);
+    const uint32_t vaddr = 2 * kTileBytes + k0 * ROWB + ((lane >> 4) & 1) * 32 + (lane & 3) * 8 + (vswz(k0) << 6);
+    bf16x8 ka[NC], va[NT][2], qf[QB][NC];
+    auto read_k = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) ka[c] = *reinterpret_cast<const bf16x8*>(s_mem + slot * kTileBytes + kaddr[c]);
+    };
+    auto read_v = [&](int t, int slot) __attribute__((always_inline)) {
+        const uint32_t a = (vaddr ^ (t << 6)) + slot * kTileBytes;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const s16x4 lo = lds_read_tr16(s_mem + a + (16 * x) * ROWB);
+            const s16x4 hi = lds_read_tr16(s_mem + a + (16 * x + 8) * ROWB);
+            const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            va[t][x] = __builtin_bit_cast(bf16x8, both);
+        }
+    };
+    float m_run[QB], mrc[QB], thr[QB], l_run[QB], lmax[QB];
+    f32x16 acc[QB][NT], s[QB], s_next[QB];
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        m_run[qb] = -INFINITY;
+        thr[qb] = -INFINITY;
+        mrc[qb] = 0.f;
+        l_run[qb] = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[qb][t] = zero;
+    }
+    auto scores = [&](f32x16& d, int qb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[c], qf[qb][c], c ? d : zero, 0, 0, 0);
+    };
+    bf16x8 pf[QB][2];
+    auto weights = [&](int qb) __attribute__((always_inline)) {
+        float pr[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) pr[i] = fast_exp2(fmaf(s[qb][i], p.c2, -mrc[qb]));
+        float sum[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = (pr[4 * i] + pr[4 * i + 1]) + (pr[4 * i + 2] + pr[4 * i + 3]);
+        l_run[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(pr[8 * x + 2 * e], pr[8 * x + 2 * e + 1]);
+            pf[qb][x] = __builtin_bit_cast(bf16x8, w);
+        }
+    };
+    auto settle = [&](int slot0) __attribute__((always_inline)) {
+        if (slot0 + kKeys > all_see) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                const int seen = P + token[qb] + 1 - slot0;
+                const uint32_t visible = (seen >= 32 ? ~0u : seen <= 0 ? 0u : (1u << seen) - 1u) >> (4 * hf);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t on = static_cast<uint32_t>(static_cast<int32_t>(visible << (31 - (8 * (i >> 2) + (i & 3)))) >> 31);
+                    s[qb][i] = __uint_as_float((on & __float_as_uint(s[qb][i])) | (~on & 0xFF800000u));
+                }
+                lmax[qb] = max16(s[qb]);
+            }
+        }
+        if (__builtin_expect(__any((lmax[0] > thr[0]) | (lmax[1] > thr[1])), 0)) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                const float m_new = fmaxf(m_run[qb], fmaxf(lmax[qb], other_half(lmax[qb])));
+                const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = m_run[qb] == -INFINITY ? 1.f : fast_exp2((m_run[qb] - m_safe) * p.c2);
+                m_run[qb] = m_new;
+                thr[qb] = m_new + p.tau;
+                mrc[qb] = m_safe * p.c2;
+                l_run[qb] *= alpha;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[qb][t] *= alpha;
+            }
+        }
+    };
+    auto meet = [&]() __attribute__((always_inline)) {     // (not __syncthreads(): it would wait for the loads that are on their way)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    // K tiles are two ahead of the one whose weights are computed, V tiles one.  raw[x] of a wavefront that brings K holds tiles x (mod 2), of one
+    // that brings V tiles x + 1 (mod 2).
+    Raw raw[2];
+    if constexpr (PAGED) {
+        take_ids(request_ids(0));
+        ids_next = request_ids(64);
+    }
+    if (is_v) {
+        load(raw[1], 0);
+        load(raw[0], 1);
+    } else {
+        load(raw[0], 0);
+        load(raw[1], 1);
+    }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const uint16_t* row = p.q + b * p.q_sb + token[qb] * p.q_sn + head[qb] * p.q_sh + 8 * hf;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) qf[qb][c] = *reinterpret_cast<const bf16x8*>(row + 16 * c);
+    }
+    if (is_v) {
+        store(raw[1], 0);
+        load(raw[1], 2);
+    } else {
+        store(raw[0], 0);
+        store(raw[1], 1);
+        load(raw[0], 2);
+        load(raw[1], 3);
+    }
+    meet();
+    read_k(0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) read_v(t, 0);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) scores(s[qb], qb);
+    read_k(1);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) lmax[qb] = max16(s[qb]);
+    // One tile: s holds its scores, lmax their maxima, va its V operands, ka the next tile's K operands.
+    auto step = [&](auto odd, auto next, int j) __attribute__((always_inline)) {
+        constexpr int ODD = decltype(odd)::value;
+        constexpr bool NEXT = decltype(next)::value;
+        settle(j * kKeys);
+        if constexpr (NEXT) {
+            store(raw[ODD], is_v ? ODD ^ 1 : ODD);         // K of tile j + 2 (none: what was there), V of tile j + 1
+            load(raw[ODD], j + (is_v ? 3 : 4));
+            scores(s_next[0], 0);
+        }
+        weights(0);
+        if constexpr (NEXT) scores(s_next[1], 1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) acc[0][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[t][x], pf[0][x], acc[0][t], 0, 0, 0);
+        weights(1);
+        if constexpr (NEXT) {
+            meet();
+            read_k(ODD);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) acc[1][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[t][x], pf[1][x], acc[1][t], 0, 0, 0);
+            if constexpr (NEXT) read_v(t, ODD ^ 1);
+        }
+        if constexpr (NEXT) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) { s[qb] = s_next[qb]; lmax[qb] = max16(s[qb]); }
+        }
+    };
+    {
+        const std::integral_constant<int, 0> even;
+        const std::integral_constant<int, 1> odd;
+        int j = 0;
+        for (; j + 2 < ntile; j += 2) {
+            step(even, std::true_type{}, j);
+            step(odd, std::true_type{}, j + 1);
+        }
+        if (j + 1 < ntile) step(even, std::true_type{}, j++);
+        step(even, std::false_type{}, j);                  // (nothing of it depends on the tile's parity)
+    }
+    if (PAGED && __any(bad_block) && lane == 0 && p.err_flag) atomicOr(p.err_flag, SPECVLM_ERR_BAD_BLOCK);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const float L = l_run[qb] + other_half(l_run[qb]);
+        const float inv = 1.f / L;
+        uint16_t* const row = p.o + b * p.o_sb + token[qb] * p.o_sn + head[qb] * p.o_sh + 8 * hf;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) store_block(acc[qb][t], inv, row + 32 * t, real[qb]);
+        if (real[qb] && p.lse && hf == 0) p.lse[(static_cast<int64_t>(b) * p.H_q + head[qb]) * p.N_max + token[qb]] = m_run[qb] * p.scale + __log2f(L) * kLn2;
+    }
+}
+
+template <int D, bool E4M3, bool PAGED>
+__global__ __launch_bounds__(kWaveWgs * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void chunk_attn_rows_kernel(ChunkParams p) {
+    attend_rows<D, E4M3, PAGED>(p);
+}
+
 template <int D, int QB, bool E4M3, bool PAGED>
 __global__ __launch_bounds__(kWaveWgs * 64) __attribute__((amdgpu_waves_per_eu(QB == 1 ? 2 : 1, QB == 1 ? 2 : 1))) void chunk_attn_kernel(ChunkParams p) {
     attend<D, QB, E4M3, PAGED>(p);
@@ -773,26 +1089,34 @@ void launch_as(const ChunkParams& p, bool e4m3, dim3 grid, hipStream_t stream) {
 }
 
 
+template <int D>
+void launch_rows(const ChunkParams& p, bool e4m3, dim3 grid, hipStream_t stream) {
+    auto* const kernel = e4m3 ? (p.g.block_table ? chunk_attn_rows_kernel<D, true, true> : chunk_attn_rows_kernel<D, true, false>)
+                              : (p.g.block_table ? chunk_attn_rows_kernel<D, false, true> : chunk_attn_rows_kernel<D, false, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(kWaveWgs * 64), 0, stream, p);
+}
+
 struct ChunkPlan {
-    int qb;                  // blocks of 32 rows per workgroup
+    int qb;                  // blocks of 32 rows per workgroup; 0: wavefronts with 64 rows each share the tiles
     int row_blocks, target;  // see ChunkParams
     int64_t workgroups;
     size_t bytes;            // workspace
 };
 
 // How a call is divided, with `bytes` of workspace.
-ChunkPlan chunk_plan(const specvlm_attn_desc& d, size_t bytes) {
+ChunkPlan chunk_plan(const specvlm_attn_desc& d, bool tree, size_t bytes) {
     ChunkPlan plan;
     const int64_t rows = static_cast<int64_t>(d.H_q / d.H_kv) * d.N_max;
-    plan.qb = rows <= 32 ? 1 : 2;
-    plan.row_blocks = static_cast<int>((rows + 32 * plan.qb - 1) / (32 * plan.qb));
+    plan.qb = rows <= 32 ? 1 : rows <= 128 || tree ? 2 : 0;
+    const int block = plan.qb ? 32 * plan.qb : kSharedRows;
+    plan.row_blocks = static_cast<int>((rows + block - 1) / block);
     const int64_t pairs = static_cast<int64_t>(d.B) * d.H_kv * plan.row_blocks;
     plan.target = 0;
     plan.workgroups = pairs;
     plan.bytes = 0;
     const int64_t capacity = d.paged ? static_cast<int64_t>(d.max_blocks_per_req) * SPECVLM_PAGE_SIZE : d.kv_capacity;
     const int64_t rounds = (capacity + kSharesRound - 1) / kSharesRound;
-    if (d.num_splits == 1 || pairs > kMostPairs || rounds <= kLeastRounds || bytes < kChunkCounterBytes) return plan;
+    if (!plan.qb || d.num_splits == 1 || pairs > kMostPairs || rounds <= kLeastRounds || bytes < kChunkCounterBytes) return plan;
     const int64_t part = static_cast<int64_t>(32) * plan.qb * (d.D + 2) * 4;
     const int64_t slots = (bytes - kChunkCounterBytes) / part;
     const int64_t want = std::max<int64_t>(plan.qb == 1 ? 512 : 256, pairs);
@@ -806,11 +1130,12 @@ ChunkPlan chunk_plan(const specvlm_attn_desc& d, size_t bytes) {
 
 }  // namespace
 
-size_t chunk_workspace_bytes(const specvlm_attn_desc& d) { return chunk_plan(d, SPECVLM_CHUNK_WORKSPACE_BYTES).bytes; }
+size_t chunk_workspace_bytes(const specvlm_attn_desc& d) { return std::max(chunk_plan(d, false, SPECVLM_CHUNK_WORKSPACE_BYTES).bytes,
+                                                                              d.N_max > SPECVLM_MAX_NODES ? 0 : chunk_plan(d, true, SPECVLM_CHUNK_WORKSPACE_BYTES).bytes); }
 
 int32_t launch_chunk_attn(const ChunkArgs& a) {
     const specvlm_attn_desc& d = a.d;
-    const ChunkPlan plan = chunk_plan(d, a.workspace_bytes);
+    const ChunkPlan plan = chunk_plan(d, a.parent != nullptr, a.workspace_bytes);
     if (plan.workgroups >= int64_t{1} << 31) return SPECVLM_INVALID_ARG;
     ChunkParams p;
     p.g = KvGeom{d.kv_stride_b, d.kv_stride_h, d.kv_stride_t, d.paged ? a.block_table : nullptr, d.max_blocks_per_req, d.num_blocks,
@@ -832,7 +1157,8 @@ int32_t launch_chunk_attn(const ChunkArgs& a) {
     p.ws_cnt = static_cast<int32_t*>(a.workspace);
     p.ws_part = static_cast<unsigned char*>(a.workspace) + kChunkCounterBytes;
     const dim3 grid(static_cast<unsigned>(plan.workgroups));
-    if (d.D == 128) plan.qb == 1 ? launch_as<128, 1>(p, a.scales != nullptr, grid, a.stream) : launch_as<128, 2>(p, a.scales != nullptr, grid, a.stream);
+    if (!plan.qb) d.D == 128 ? launch_rows<128>(p, a.scales != nullptr, grid, a.stream) : launch_rows<64>(p, a.scales != nullptr, grid, a.stream);
+    else if (d.D == 128) plan.qb == 1 ? launch_as<128, 1>(p, a.scales != nullptr, grid, a.stream) : launch_as<128, 2>(p, a.scales != nullptr, grid, a.stream);
     else plan.qb == 1 ? launch_as<64, 1>(p, a.scales != nullptr, grid, a.stream) : launch_as<64, 2>(p, a.scales != nullptr, grid, a.stream);
     return check_launch();
 }

@@ -139,3 +139,12 @@ def test_block_ids_outside_the_pool(sv, dtype):
         err = i32([0])
         out = sv.specvlm_chunk_attn(q, cache.k, cache.v, i32([97, 97]), block_table=table, scales=cache.scales, err_flag=err)
         assert int(err) == 16 and torch.equal(out[1], good[1])
+
+
+@kinds
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,G,N,prefix,new", [(4, 4, 300, [0], [300]), (8, 2, 129, [63, 0, 1000], [129, 128, 1]), (3, 1, 1000, [0, 500], [1000, 333]),
+                                              (2, 2, 2050, [31], [2050]), (5, 1, 200, [2111, 0], [200, 52]), (8, 1, 33, [1, 2, 3], [33, 32, 0]),
+                                              (1, 1, 512, [2000], [256]), (7, 1, 1100, [40], [1100])])
+def test_long_chunks(sv, dtype, paged, D, H, G, N, prefix, new):
+    run(sv, N + H, H, G, D, N, prefix, new, dtype, paged, fused=True)

@@ -4,15 +4,21 @@ import os
 import re
 import subprocess
 
+import pytest
+
 TICKET = re.compile(r'atomicrmw add ptr.* syncscope\("agent(?:-one-as)?"\) monotonic')
 ORDERS = re.compile(r"\bfence\b|~\{memory\}")
 READS = re.compile(r"\bload atomic\b|@llvm\.amdgcn\.raw\.ptr\.buffer\.load")
 
 
-def test_reads_behind_the_ticket(tmp_path):
+SOURCES = ["chunk_attn.hip", "chunk_rows.hip"]
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_reads_behind_the_ticket(tmp_path, source):
     from paper_2509_11815_amd import build
     out = str(tmp_path / "k.ll")
-    subprocess.run([build._hipcc(), *build.HIPCC_FLAGS, "--cuda-device-only", "-S", "-emit-llvm", "-o", out, os.path.join(build.CSRC, "chunk_attn.hip")], check=True, capture_output=True)
+    subprocess.run([build._hipcc(), *build.HIPCC_FLAGS, "--cuda-device-only", "-S", "-emit-llvm", "-o", out, os.path.join(build.CSRC, source)], check=True, capture_output=True)
     with open(out) as f:
         lines = f.read().split("\n")
     found = 0
@@ -28,9 +34,10 @@ def test_reads_behind_the_ticket(tmp_path):
     assert found >= 8
 
 
-def test_nothing_spills():
+@pytest.mark.parametrize("source", SOURCES)
+def test_nothing_spills(source):
     from paper_2509_11815_amd import build
-    usage = build.kernel_resource_usage("chunk_attn.hip")
+    usage = build.kernel_resource_usage(source)
     kernels = {k: v for k, v in usage.items() if "_kernel" in k}
     assert len(kernels) >= 8, sorted(usage)
     for name, u in kernels.items():

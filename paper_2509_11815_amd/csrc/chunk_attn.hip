@@ -32,26 +32,23 @@ __device__ __forceinline__ void attend32(const ChunkParams& p) {
     __shared__ float s_m[kWaveWgs][32];
     __shared__ float s_l[kWaveWgs][32];
 
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
     Item it;
-    if (!find_item<32>(p, lane, it)) return;
+    if (!find_item<32, 2, 4>(p, lane, it)) return;
     it = uniform(it);
     const int b = it.b, hk = it.hk, n = it.n, P = it.P, S = P + n;
     const int row0 = it.rb * 32;
-    const Rows<1> rows(p, hk, n, row0);
+    const Rows<1> rows(p, hk, n, row0, l32);
     unsigned long long anc[1] = {};
     if (p.parent && !ancestors(p, it, lane, rows.token, anc)) return;
     const int first_token = divide(row0, p.magic_group);
-    const int last_token = min(static_cast<int>(divide(row0 + 31, p.magic_group)), n - 1);
+    const int last_token = Work<ChunkParams, 32, false>::last_token(p, n, it.rb);
     const int all_see = p.parent ? P : P + first_token + 1;          // slots that every row of the block sees
     const int end = p.parent ? S : P + last_token + 1;               // slots that some row sees
-    // Tiles of this range of keys: whole rounds of the request, up to the block's end; this wavefront's stream has every fourth.
-    const int rounds = static_cast<int>((static_cast<uint32_t>(S - 1) + kSharesRound) / kSharesRound);
-    const int first_round = it.x * rounds / it.c, next_round = (it.x + 1) * rounds / it.c;
-    const int ntile = min((end - 1) / kKeys + 1, next_round * kWaveWgs);
-    const int tile0 = first_round * kWaveWgs + wave;
+    // Tiles of this segment, up to the block's end; this wavefront's stream has every fourth.
+    const int ntile = min((end - 1) / kKeys + 1, it.to * kWaveWgs);
+    const int tile0 = it.from * kWaveWgs + wave;
     const int my_tiles = tile0 < ntile ? (ntile - tile0 + kWaveWgs - 1) / kWaveWgs : 0;
 
     // ---- tile fetch -------------------------------------------------------------------------
@@ -245,7 +242,7 @@ void launch_few(const ChunkParams& p, bool e4m3, dim3 grid, hipStream_t stream) 
 
 struct ChunkPlan {
     int qb;                  // blocks of 32 rows per workgroup; 0: wavefronts with 64 rows each share the tiles
-    int row_blocks, target;  // see ChunkParams
+    int row_blocks, target, places;          // see ChunkParams
     int64_t workgroups;
     size_t bytes;            // workspace
 };
@@ -258,20 +255,18 @@ ChunkPlan chunk_plan(const specvlm_attn_desc& d, bool tree, size_t bytes) {
     const int block = plan.qb ? 32 * plan.qb : kSharedRows;
     plan.row_blocks = static_cast<int>((rows + block - 1) / block);
     const int64_t pairs = static_cast<int64_t>(d.B) * d.H_kv * plan.row_blocks;
-    plan.target = 0;
+    plan.target = plan.places = 0;
     plan.workgroups = pairs;
     plan.bytes = 0;
-    const int64_t capacity = d.paged ? static_cast<int64_t>(d.max_blocks_per_req) * SPECVLM_PAGE_SIZE : d.kv_capacity;
-    const int64_t rounds = (capacity + kSharesRound - 1) / kSharesRound;
-    if (!plan.qb || d.num_splits == 1 || pairs > kMostPairs || rounds <= kLeastRounds || bytes < kChunkCounterBytes) return plan;
-    const int64_t part = static_cast<int64_t>(32) * plan.qb * (d.D + 2) * 4;
-    const int64_t slots = (bytes - kChunkCounterBytes) / part;
-    const int64_t want = std::max<int64_t>(plan.qb == 1 ? 512 : 256, pairs);
-    const int64_t most = std::min(want, pairs * std::min<int64_t>(kMostColumns, (rounds + kLeastRounds - 1) / kLeastRounds));
-    if (slots < pairs) return plan;
-    plan.target = static_cast<int>(std::min(most, slots));
-    plan.workgroups = (plan.target + 7) / 8 * 8;
-    plan.bytes = kChunkCounterBytes + plan.target * part;
+    const int64_t slots = bytes < kChunkCounterBytes ? 0 : (bytes - kChunkCounterBytes) / (2 * part_bytes(block, d.D));
+    if (d.num_splits == 1 || pairs > kMostPairs || slots < 8) return plan;
+    // A place for a workgroup on every compute unit, for two of 32 rows.  Key streams: a part for every place, up to two or three times as many
+    plan.places = plan.qb == 1 ? 512 : 256;
+    const int64_t most = std::min<int64_t>(!plan.qb ? plan.places : std::max<int64_t>((plan.qb == 1 ? 2 : 3) * plan.places, pairs), slots);
+    if (plan.qb && most < pairs) return plan;
+    plan.target = static_cast<int>(most);
+    plan.workgroups = (std::max<int64_t>(plan.target, plan.qb ? 0 : pairs) + 7) / 8 * 8;
+    plan.bytes = kChunkCounterBytes + static_cast<size_t>(plan.target) * 2 * part_bytes(block, d.D);
     return plan;
 }
 
@@ -301,6 +296,7 @@ int32_t launch_chunk_attn(const ChunkArgs& a) {
     p.c2 = a.scale * kLog2e;
     p.tau = std::fmin(kTau / p.c2, 1e30f);
     p.target = plan.target;
+    p.places = plan.places;
     p.ws_cnt = static_cast<int32_t*>(a.workspace);
     p.ws_part = static_cast<unsigned char*>(a.workspace) + kChunkCounterBytes;
     const unsigned workgroups = static_cast<unsigned>(plan.workgroups);

@@ -4,6 +4,7 @@
 
 #include "attn_common.hpp"
 #include "attn_rows.hpp"
+#include "chunk_share.hpp"
 #include "wave_ops.hpp"
 
 namespace specvlm {
@@ -21,153 +22,35 @@ struct ChunkParams {
     int B, N_max, H_q, H_kv, group, row_blocks;
     uint32_t magic_group;
     float scale, c2, tau;                    // softmax scale; times log2 e; how far a score may lie above the reference
-    int target;                              // workgroups to divide the keys among, 0: one range of keys for every (request, KV head, row block)
-    int32_t* ws_cnt;                         // [pairs] arrival tickets, kCounterStride words apart, zero between calls
-    unsigned char* ws_part;                  // [items] partial results, see merge_ranges()
+    int target, places;                      // workgroups to divide the call among at most (0: one for every (request, KV head, row block)), and at once
+    int32_t* ws_cnt;                         // [items] arrival tickets, kCounterStride words apart, zero between calls
+    unsigned char* ws_part;                  // two partial results a workgroup
 };
 
-// The kernels with 64 rows a wavefront (chunk_rows.hip); `shared`: 256 rows a workgroup, no ranges of keys.
+// The kernels with 64 rows a wavefront (chunk_rows.hip); `shared`: 256 rows a workgroup.
 void launch_chunk_rows(const ChunkParams& p, int D, bool e4m3, bool shared, unsigned workgroups, hipStream_t stream);
 
 constexpr int kSharedRows = 256;             // rows of a workgroup whose wavefronts share tiles
-constexpr int kLeastRounds = 2;              // rounds a range of keys has at least: below that the meeting of the partial results costs more
-constexpr int kMostColumns = 64;             // ranges of keys of one (request, KV head, row block)
-constexpr int kMostPairs = 1024;             // (request, KV head, row block)s of a call whose keys are divided: more fill the chip by themselves
+static_assert(kChunkKeys == kKeys, "keys per tile");
+constexpr int kLeastRounds = 2;              // rounds a part has at least where the keys of an item are divided
+constexpr int kMostPairs = 4096;             // (request, KV head, row block)s of a call that is divided: more even out by themselves
 constexpr size_t kChunkCounterBytes = kMostPairs * kCounterStride * 4;     // tickets: a 128-byte line each
+constexpr int part_bytes(int rows, int D) { return rows * (D + 2) * 4; }   // accumulators, then a (maximum, sum) pair a row, in fp32
 
 namespace {        // (device functions of each file's kernels)
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 
-// A workgroup's part of the call: column x of the c ranges of keys of (request, KV head, row block).
-struct Item { int b, hk, rb, x, c, n, P, index; };
-
-// The same in scalar registers, where the compiler does not see that all lanes agree.
-__device__ __forceinline__ Item uniform(const Item& it) {
-    auto u = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-    return Item{u(it.b), u(it.hk), u(it.rb), u(it.x), u(it.c), u(it.n), u(it.P), u(it.index)};
-}
-
 __device__ __forceinline__ int wave_sum_int(int x) {
     x = row_sum(x);
     return (__builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16)) + (__builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48));
 }
 
-// Sum over the lanes up to this one.
-__device__ __forceinline__ int wave_scan(int x, int lane) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);           // row_shr:1, zero where there is none
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
-    const int a = __builtin_amdgcn_readlane(x, 15), b = a + __builtin_amdgcn_readlane(x, 31), c = b + __builtin_amdgcn_readlane(x, 47);
-    return x + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
-}
+static_assert(SPECVLM_ERR_BAD_NUM_NODES == 2 && SPECVLM_ERR_BAD_LENGTH == 4, "chunk_length_error()");
+__device__ __forceinline__ int length_error(const ChunkParams& p, int n, int P) { return chunk_length_error(n, P, p.N_max, p.g.capacity); }
 
-__device__ __forceinline__ int length_error(const ChunkParams& p, int n, int P) {
-    return n < 0 || n > p.N_max ? SPECVLM_ERR_BAD_NUM_NODES : P < 0 || P > p.g.capacity - n ? SPECVLM_ERR_BAD_LENGTH : 0;
-}
-
-// A 32 x 32 block of O^T (dims 8 (i / 4) + 4 (lane / 32) + i % 4 of the lane's row) times inv, as bf16; `to`: the row's dims 8 (lane / 32) ..
-__device__ __forceinline__ void store_block(const f32x16& a, float inv, uint16_t* to, bool live) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {                          // 16 dims: registers 8u .. 8u + 7
-        uint32_t x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = pack_bf16x2(a[8 * u + 2 * i] * inv, a[8 * u + 2 * i + 1] * inv);
-        // the halves of the wavefront hold dims 0-3, 8-11 and 4-7, 12-15: the lower keeps 0-7, the upper 8-15
-        const auto r0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
-        const auto r1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
-        if (live) *reinterpret_cast<u32x4*>(to + 16 * u) = u32x4{r0[0], r1[0], r0[1], r1[1]};
-    }
-}
-
-// What a workgroup has to do, worked out by each from the lengths, which the host does not know.  Every range of keys of every (request, KV
-// head, row block) gets about the same number of rounds (a round: a tile of every wavefront): the least `len` for which the ranges are no
-// more than `target` workgroups (or one each).  Returns false where there is nothing to do.
-template <int ROWS>
-__device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& it) {
-    typedef const __attribute__((address_space(4))) int32_t* const_i32;
-    if (!p.target) {
-        const uint32_t pair = blockIdx.x / static_cast<uint32_t>(p.row_blocks);
-        it.rb = blockIdx.x - pair * p.row_blocks;
-        it.b = pair / static_cast<uint32_t>(p.H_kv);
-        it.hk = pair - it.b * p.H_kv;
-        it.n = p.num_new ? ((const_i32)p.num_new)[it.b] : p.N_max;
-        it.P = ((const_i32)p.prefix_len)[it.b];
-        it.x = 0;
-        it.c = 1;
-        it.index = blockIdx.x;
-        if (const int err = length_error(p, it.n, it.P)) {
-            if (it.rb == 0 && it.hk == 0 && threadIdx.x == 0 && p.err_flag) atomicOr(p.err_flag, err);
-            return false;
-        }
-        return it.rb * ROWS < p.group * it.n;
-    }
-    int n = 0, P = 0, rounds = 0, units = 0;               // of request b0 + lane
-    auto look = [&](int b0, bool report) __attribute__((always_inline)) {
-        const int b = b0 + lane;
-        rounds = units = 0;
-        if (b < p.B) {
-            n = p.num_new ? p.num_new[b] : p.N_max;
-            P = p.prefix_len[b];
-            if (const int err = length_error(p, n, P)) {
-                if (report && p.err_flag) atomicOr(p.err_flag, err);
-            } else if (n) {
-                rounds = static_cast<int>((static_cast<uint32_t>(P + n - 1) + kSharesRound) / kSharesRound);
-                units = (p.group * n + ROWS - 1) / ROWS * p.H_kv;
-            }
-        }
-    };
-    // (more than 64 requests: looked at 64 at a time, again for every pass)
-    const bool first = blockIdx.x == 0 && threadIdx.x < 64;
-    float total = 0.f;
-    int pairs = 0, longest = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        look(b0, first);
-        total += wave_sum(static_cast<float>(rounds) * units);
-        pairs += wave_sum_int(units);
-        longest = max(longest, static_cast<int>(wave_max(static_cast<float>(rounds))));      // (up to 2^24: exact)
-    }
-    const int most = max(p.target, pairs);
-    int len = max(static_cast<int>(ceilf(total / p.target)), max(kLeastRounds, (longest + kMostColumns - 1) / kMostColumns));
-    int all;
-    for (;; len += 1 + (len >> 4)) {
-        all = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 64) {
-            if (p.B > 64) look(b0, false);
-            all += wave_sum_int(units * ((rounds + len - 1) / len));
-        }
-        if (all <= most || len >= longest) break;
-    }
-    // every XCD has a contiguous range of the items, so that the row blocks of a head's keys share an L2
-    const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, share = all >> 3, more = all & 7;
-    if (place >= share + (xcd < more)) return false;
-    it.index = xcd * share + min(xcd, more) + place;
-    int before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        if (p.B > 64) look(b0, false);
-        const int mine = units * ((rounds + len - 1) / len), upto = before + wave_scan(mine, lane);
-        const unsigned long long here = __ballot(it.index < upto);
-        if (here) {
-            const int at = __builtin_ctzll(here);
-            it.b = b0 + at;
-            it.n = __builtin_amdgcn_readlane(n, at);
-            it.P = __builtin_amdgcn_readlane(P, at);
-            const uint32_t local = it.index - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
-            const uint32_t units_of = __builtin_amdgcn_readlane(units, at), blocks = units_of / static_cast<uint32_t>(p.H_kv);
-            it.c = (__builtin_amdgcn_readlane(rounds, at) + len - 1) / len;
-            it.x = local / units_of;
-            const uint32_t rest = local - it.x * units_of;
-            it.hk = rest / blocks;
-            it.rb = rest - it.hk * blocks;
-            return true;
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
-    }
-    return false;
-}
-
+// The greatest of sixteen scores, NaN where one is.
 __device__ __forceinline__ float max16(const f32x16& a) {
     auto max3 = [](float x, float y, float z) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z); };
     const float u = max3(a[0], a[1], a[2]), v = max3(a[3], a[4], a[5]), w = max3(a[6], a[7], a[8]), x = max3(a[9], a[10], a[11]);
@@ -185,50 +68,278 @@ __device__ __forceinline__ float other_half(float x) {
 // LDS traffic between lanes of one wavefront needs no wait (it is in order) but must stay in order.
 __device__ __forceinline__ void wave_order() { asm volatile("" ::: "memory"); }
 
-// Items between two ranges of keys of one (request, KV head, row block): find_item() puts the request's (head, block) pairs in between.
-__device__ __forceinline__ int step_of(const ChunkParams& p, const Item& it, int rows) { return (p.group * it.n + rows - 1) / rows * p.H_kv; }
+// A 32 x 32 block of O^T (dims 8 (i / 4) + 4 (lane / 32) + i % 4 of the lane's row) times inv, as bf16; `to`: the row's dims 8 (lane / 32) ..
+__device__ __forceinline__ void store_block(const f32x16& a, float inv, uint16_t* to, bool live) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {                          // 16 dims: registers 8u .. 8u + 7
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = pack_bf16x2(a[8 * u + 2 * i] * inv, a[8 * u + 2 * i + 1] * inv);
+        // the halves of the wavefront hold dims 0-3, 8-11 and 4-7, 12-15: the lower keeps 0-7, the upper 8-15
+        const auto r0 = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
+        const auto r1 = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+        if (live) *reinterpret_cast<u32x4*>(to + 16 * u) = u32x4{r0[0], r1[0], r0[1], r1[1]};
+    }
+}
 
-// The partial results of an item's ranges of keys, in their order, by the 256 threads of the workgroup that came last.  A unit is four head
-// dims of a row; where the block has few rows, threads share a unit's ranges and meet in LDS.
+// The same item in scalar registers.
+__device__ __forceinline__ Item uniform(const Item& x) {
+    return Item{u(x.b), u(x.hk), u(x.rb), u(x.n), u(x.P), u(x.from), u(x.to), u(x.steps), u(x.part), u(x.parts), u(x.first)};
+}
+
+// The thread's number, anew: what a segment's code derives from it is worked out there and not kept in registers from one segment to the next.
+__device__ __forceinline__ int this_thread() {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    return tid;
+}
+
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int x, int lane) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);           // row_shr:1, zero where there is none
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    const int a = __builtin_amdgcn_readlane(x, 15), b = a + __builtin_amdgcn_readlane(x, 31), c = b + __builtin_amdgcn_readlane(x, 47);
+    return x + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
+}
+
+// Calls whose workgroups have key streams: one segment each, worked out by every workgroup from the lengths.  All parts of all items get about
+// the same number of rounds (a round: a tile of every stream, 128 keys).  Returns false where there is nothing to do.
+// (Equal stretches as in Share leave no workgroup with more than the mean, but most with the end of one item and the beginning of the next, and
+// each segment is a chain of latencies: one token over 768 keys of 32 heads 10.9 -> 19.5 us, sixteen over 64 - 16383 36.7 -> 42.4.)
+template <int ROWS, int kTurns, int kFixed>
+__device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& it) {
+    typedef const __attribute__((address_space(4))) int32_t* const_i32;
+    if (!p.target) {
+        const uint32_t pair = blockIdx.x / static_cast<uint32_t>(p.row_blocks);
+        it.rb = blockIdx.x - pair * p.row_blocks;
+        it.b = pair / static_cast<uint32_t>(p.H_kv);
+        it.hk = pair - it.b * p.H_kv;
+        it.n = p.num_new ? ((const_i32)p.num_new)[it.b] : p.N_max;
+        it.P = ((const_i32)p.prefix_len)[it.b];
+        it.part = it.first = 0;
+        it.parts = 1;
+        if (const int err = length_error(p, it.n, it.P)) {
+            if (it.rb == 0 && it.hk == 0 && threadIdx.x == 0 && p.err_flag) atomicOr(p.err_flag, err);
+            return false;
+        }
+        if (it.rb * ROWS >= p.group * it.n) return false;
+        it.from = 0;
+        it.to = it.steps = Work<ChunkParams, ROWS, false>::rounds(it.P, it.n);
+        return true;
+    }
+    int n = 0, P = 0, rounds = 0, units = 0;               // of request b0 + lane
+    auto look = [&](int b0, bool report) __attribute__((always_inline)) {
+        const int b = b0 + lane;
+        rounds = units = 0;
+        if (b < p.B) {
+            n = p.num_new ? p.num_new[b] : p.N_max;
+            P = p.prefix_len[b];
+            if (const int err = length_error(p, n, P)) {
+                if (report && p.err_flag) atomicOr(p.err_flag, err);
+            } else if (n) {
+                rounds = Work<ChunkParams, ROWS, false>::rounds(P, n);
+                units = Work<ChunkParams, ROWS, false>::blocks(p, n) * p.H_kv;
+            }
+        }
+    };
+    // (more than 64 requests: looked at 64 at a time, again for every pass)
+    const bool first = blockIdx.x == 0 && threadIdx.x < 64;
+    float total = 0.f;
+    int pairs = 0, longest = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        look(b0, first);
+        total += wave_sum(static_cast<float>(rounds) * units);
+        pairs += wave_sum_int(units);
+        longest = max(longest, static_cast<int>(wave_max(static_cast<float>(rounds))));      // (up to 2^24: exact)
+    }
+    // The least number of rounds a part for which the parts are no more than one workgroup for every place on the chip (or one part an item).
+    // Where that leaves places empty because items have few rounds, twice or three times as many shorter parts: kFixed rounds are what a part costs beside its own.
+    auto parts_of = [&](int len) __attribute__((always_inline)) {
+        int sum = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            if (p.B > 64) look(b0, false);
+            sum += wave_sum_int(units * ((rounds + len - 1) / len));
+        }
+        return sum;
+    };
+    const int shortest = max(kLeastRounds, (longest + kMostParts - 1) / kMostParts);
+    int len = longest, all = pairs, best = 1 << 30;
+    for (int turns = 1; turns <= kTurns; ++turns) {
+        const int most = min(turns * p.places, p.target);
+        int l = max(static_cast<int>(ceilf(total / most)), shortest), sum;
+        for (; (sum = parts_of(l)) > most && l < longest; l += 1 + (l >> 4)) {}
+        l = min(l, longest);
+        const int cost = (sum + p.places - 1) / p.places * (l + kFixed);
+        if (cost < best) { best = cost; len = l; all = sum; }
+        if (l <= shortest) break;
+    }
+    // every XCD has a contiguous range of the items, so that the row blocks of a head's keys share an L2
+    const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, share = all >> 3, more = all & 7;
+    if (place >= share + (xcd < more)) return false;
+    const int index = xcd * share + min(xcd, more) + place;
+    int before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        if (p.B > 64) look(b0, false);
+        const int mine = units * ((rounds + len - 1) / len), upto = before + wave_scan(mine, lane);
+        const unsigned long long here = __ballot(index < upto);
+        if (here) {
+            const int at = __builtin_ctzll(here);
+            it.b = b0 + at;
+            it.n = __builtin_amdgcn_readlane(n, at);
+            it.P = __builtin_amdgcn_readlane(P, at);
+            const uint32_t local = index - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(mine, at));
+            const uint32_t blocks = static_cast<uint32_t>(__builtin_amdgcn_readlane(units, at)) / static_cast<uint32_t>(p.H_kv);
+            it.steps = __builtin_amdgcn_readlane(rounds, at);
+            it.parts = (it.steps + len - 1) / len;
+            const uint32_t item = local / static_cast<uint32_t>(it.parts);
+            it.part = local - item * it.parts;
+            it.first = index - it.part;
+            it.hk = item / blocks;
+            it.rb = item - it.hk * blocks;
+            it.from = static_cast<int>(static_cast<uint32_t>(it.part) * it.steps / it.parts);
+            it.to = static_cast<int>((static_cast<uint32_t>(it.part) + 1) * it.steps / it.parts);
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// Where a workgroup's share begins.  False: nothing to do.
+template <int ROWS, bool TILES>
+__device__ __forceinline__ bool begin_share(Share<ChunkParams, ROWS, TILES>& s, int lane) {
+    using W = Work<ChunkParams, ROWS, TILES>;
+    const ChunkParams& p = s.p;
+    s.done = false;
+    s.skip = 0;
+    // An item a workgroup, the blocks with the most keys first
+    auto undivided = [&](bool report) __attribute__((always_inline)) {
+        s.whole = true;
+        const uint32_t pairs = static_cast<uint32_t>(p.B) * p.H_kv;
+        const uint32_t level = blockIdx.x / pairs, pair = blockIdx.x - level * pairs;
+        s.rb = p.row_blocks - 1 - level;
+        if (s.rb < 0) return false;
+        s.b = pair / static_cast<uint32_t>(p.H_kv);
+        s.hk = pair - s.b * p.H_kv;
+        const int n = p.num_new ? p.num_new[s.b] : p.N_max, P = p.prefix_len[s.b];
+        if (const int err = length_error(p, n, P)) {
+            if (report && s.rb == 0 && s.hk == 0 && threadIdx.x == 0 && p.err_flag) atomicOr(p.err_flag, err);
+            return false;
+        }
+        return s.request(s.b, u(n), u(P)) && s.rb < s.blocks;
+    };
+    if (!p.target) return undivided(true);
+    s.whole = false;
+    const bool report = blockIdx.x == 0 && threadIdx.x < 64 && p.err_flag;
+    // lane i: request b0 + i; more than 64 requests are looked at 64 at a time, and once more for the place
+    double weight = 0.0, sum = 0.0;
+    int items = 0, n = 0, P = 0;
+    float heaviest = 0.f, lightest = INFINITY;             // last blocks of the requests
+    auto look = [&](int b0, bool first) __attribute__((always_inline)) {
+        const int at = b0 + lane;
+        int here = 0;
+        double most = 0.0;
+        weight = 0.0;
+        if (at < p.B) {
+            n = p.num_new ? p.num_new[at] : p.N_max;
+            P = p.prefix_len[at];
+            if (const int err = length_error(p, n, P)) {
+                if (first && report) atomicOr(p.err_flag, err);
+            } else if (n) {
+                const int blocks = W::blocks(p, n);
+                here = blocks * p.H_kv;
+                weight = W::before(p, n, P, blocks) * p.H_kv;
+                if (first) most = W::weight(p, n, P, blocks - 1);
+            }
+        }
+        if (first) {
+            items += wave_sum_int(here);
+            heaviest = fmaxf(heaviest, wave_max(here ? static_cast<float>(most) : 0.f));
+            lightest = fminf(lightest, -wave_max(here ? -static_cast<float>(most) : -INFINITY));
+        }
+    };
+    // Sum over the lanes up to this one (exact: whole numbers)
+    auto scan = [&](double x) __attribute__((always_inline)) {
+        for (int d = 1; d < min(64, p.B); d *= 2) {
+            const double other = __shfl_up(x, d);
+            if (lane >= d) x += other;
+        }
+        return x;
+    };
+    double upto = 0.0;
+    const int last_lane = min(64, p.B) - 1;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        look(b0, true);
+        upto = scan(weight);
+        sum += __shfl(upto, last_lane);
+    }
+    if (!items) return false;
+    s.divide_line(sum, items, heaviest);
+    if (s.undivided_is_faster(sum, items, heaviest, lightest == heaviest)) return undivided(false);
+    s.mine = s.stretch_of(blockIdx.x);
+    if (s.mine < 0) return false;
+    const double at = s.cut(s.mine);
+    double past = 0.0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        if (p.B > 64) {
+            look(b0, false);
+            upto = scan(weight);
+        }
+        const unsigned long long here = __ballot(lane <= last_lane && past + upto > at);
+        if (here || b0 + 64 >= p.B) {
+            const int to = here ? __builtin_ctzll(here) : last_lane;
+            if (!s.request(u(b0 + to), __builtin_amdgcn_readlane(n, to), __builtin_amdgcn_readlane(P, to))) return false;  // (cannot be: the line ends with an item)
+            s.find_block(past + __shfl(upto - weight, to));
+            return !s.done;
+        }
+        past += __shfl(upto, last_lane);
+    }
+    return false;
+}
+
+// The parts of an item, in their order, by the 256 threads of the workgroup that came last.  A unit is four head dims of a row; where the
+// block has few rows, threads share a unit's parts and meet in LDS. 
 template <int D, int ROWS>
-__device__ __forceinline__ void merge_ranges(const ChunkParams& p, const Item& it, const unsigned char* parts, int64_t part_step, unsigned char* lds) {
+__device__ __forceinline__ void merge_parts(const ChunkParams& p, const Item& it, unsigned char* lds) {
     constexpr int kCoherent = 16;                          // device-coherent (sc1) loads, which the compiler counts
-    constexpr int NT = D / 32;
-    const int tid = threadIdx.x, row0 = it.rb * ROWS;
+    constexpr int NT = D / 32, kPart = part_bytes(ROWS, D);
+    const int tid = this_thread(), row0 = it.rb * ROWS;
     const int rows = min(ROWS, p.group * it.n - row0);
-    float* const s_w = reinterpret_cast<float*>(lds);      // [rows][c] maxima, then weights
-    float* const s_inv = s_w + ROWS * kMostColumns;        // [rows]
+    float* const s_w = reinterpret_cast<float*>(lds);      // [rows][kMostParts] weights
+    float* const s_inv = s_w + ROWS * kMostParts;        // [rows]
     float* const s_sum = s_inv + ROWS;                     // [256][4]
     auto load = [&](int64_t off, auto wide) __attribute__((always_inline)) {
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(parts), 0, 0x7FFFFFFF, 0x00027000);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(p.ws_part, 0, 0x7FFFFFFF, 0x00027000);
         if constexpr (decltype(wide)::value) return __builtin_amdgcn_raw_buffer_load_b128(rsrc, static_cast<int>(off), 0, kCoherent);
         else return __builtin_amdgcn_raw_buffer_load_b64(rsrc, static_cast<int>(off), 0, kCoherent);
     };
-    // eight threads a row: its maximum over the ranges, their weights, the sum
+    // eight threads a row: its maximum over the parts, their weights, the sum
     for (int r = tid >> 3; r < rows; r += 32) {
         const int i0 = tid & 7;
-        float m[kMostColumns / 8], l[kMostColumns / 8], M = -INFINITY, L = 0.f;
+        float m[kMostParts / 8], l[kMostParts / 8], M = -INFINITY, L = 0.f;
 #pragma unroll
-        for (int k = 0; k < kMostColumns / 8; ++k) {
+        for (int k = 0; k < kMostParts / 8; ++k) {
             m[k] = -INFINITY;
             l[k] = 0.f;
-            if (i0 + 8 * k < it.c) {
-                const u32x2 ml = load((i0 + 8 * k) * part_step + ROWS * D * 4 + r * 8, std::false_type{});
+            if (i0 + 8 * k < it.parts) {
+                const u32x2 ml = load(part_at(it, i0 + 8 * k, kPart) + ROWS * D * 4 + r * 8, std::false_type{});
                 m[k] = __uint_as_float(ml[0]);
                 l[k] = __uint_as_float(ml[1]);
             }
         }
 #pragma unroll
-        for (int k = 0; k < kMostColumns / 8; ++k) M = __builtin_elementwise_maximum(M, m[k]);
+        for (int k = 0; k < kMostParts / 8; ++k) M = __builtin_elementwise_maximum(M, m[k]);
         M = __builtin_elementwise_maximum(M, dpp<0x141>(M));
         M = __builtin_elementwise_maximum(M, dpp<0x4E>(M));
         M = __builtin_elementwise_maximum(M, dpp<0xB1>(M));
         const float m_safe = M == -INFINITY ? 0.f : M;
 #pragma unroll
-        for (int k = 0; k < kMostColumns / 8; ++k) {
+        for (int k = 0; k < kMostParts / 8; ++k) {
             const float w = fast_exp2((m[k] - m_safe) * p.c2);
             L += l[k] * w;
-            if (i0 + 8 * k < it.c) s_w[r * kMostColumns + i0 + 8 * k] = w;
+            if (i0 + 8 * k < it.parts) s_w[r * kMostParts + i0 + 8 * k] = w;
         }
         L += dpp<0x141>(L);
         L += dpp<0x4E>(L);
@@ -259,13 +370,13 @@ __device__ __forceinline__ void merge_ranges(const ChunkParams& p, const Item& i
             const int off = ((block * 4 + u) * 64 + hf * 32 + r) * 16;
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
             constexpr int BATCH = 8;
-            for (int i = part; i < it.c; i += share * BATCH) {
+            for (int i = part; i < it.parts; i += share * BATCH) {
                 u32x4 x[BATCH];
 #pragma unroll
-                for (int k = 0; k < BATCH; ++k) x[k] = load(min(i + k * share, it.c - 1) * part_step + off, std::true_type{});
+                for (int k = 0; k < BATCH; ++k) x[k] = load(part_at(it, min(i + k * share, it.parts - 1), kPart) + off, std::true_type{});
 #pragma unroll
                 for (int k = 0; k < BATCH; ++k) {
-                    const float w = i + k * share < it.c ? s_w[(q + r) * kMostColumns + i + k * share] : 0.f;
+                    const float w = i + k * share < it.parts ? s_w[(q + r) * kMostParts + i + k * share] : 0.f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sum[e] = fmaf(__uint_as_float(x[k][e]), w, sum[e]);
                 }
@@ -292,15 +403,48 @@ __device__ __forceinline__ void merge_ranges(const ChunkParams& p, const Item& i
     }
 }
 
+// The workgroup's next segment; false: there is none.  One barrier, behind which LDS is free for it.
+struct Segments {
+    ShareState state;
+    Item item[2];
+    int some[2];
+};
+template <int ROWS, bool TILES>
+__device__ __forceinline__ bool next_segment(const ChunkParams& p, Segments& lds, int turn, Item& it) {
+    const int lane = this_thread() & 63, at = turn & 1;    // (two places: a slow wavefront may still read the last one)
+    if (threadIdx.x < 64) {
+        Share<ChunkParams, ROWS, TILES> share(p);
+        Item found;
+        bool some;
+        if (turn) {
+            share.take(lds.state);
+            some = share.next(found);
+        } else {
+            some = begin_share(share, lane) && share.next(found);
+        }
+        if (lane == 0) {
+            if (some) {
+                lds.item[at] = found;
+                share.keep(lds.state);
+            }
+            lds.some[at] = some;
+        }
+    }
+    __syncthreads();
+    if (!u(lds.some[at])) return false;
+    it = uniform(lds.item[at]);
+    return true;
+}
+
 // Rows of a lane's blocks of 32: token and head; rows that do not exist count as the last token's.
 template <int QB>
 struct Rows {
     int token[QB], head[QB];
     bool real[QB];
-    __device__ __forceinline__ Rows(const ChunkParams& p, int hk, int n, int row0) {
+    __device__ __forceinline__ Rows(const ChunkParams& p, int hk, int n, int row0, int l32) {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-            const int R = row0 + qb * 32 + (threadIdx.x & 31);
+            const int R = row0 + qb * 32 + l32;
             token[qb] = divide(R, p.magic_group);
             head[qb] = hk * p.group + R - token[qb] * p.group;
             real[qb] = token[qb] < n;
@@ -315,7 +459,7 @@ __device__ __forceinline__ bool ancestors(const ChunkParams& p, const Item& it, 
     const int par = lane < it.n ? p.parent[static_cast<int64_t>(it.b) * p.N_max + lane] : -1;
     const bool bad_par = lane < it.n && (lane == 0 ? par != -1 : (par < 0 || par >= lane));
     if (__any(bad_par)) {                                  // the same in every workgroup of the request
-        if (it.rb == 0 && it.hk == 0 && it.x == 0 && threadIdx.x == 0 && p.err_flag) atomicOr(p.err_flag, SPECVLM_ERR_BAD_PARENT);
+        if (it.rb == 0 && it.hk == 0 && it.part == 0 && threadIdx.x == 0 && p.err_flag) atomicOr(p.err_flag, SPECVLM_ERR_BAD_PARENT);
         return false;
     }
     uint32_t mlo = lane < 32 ? 1u << (lane & 31) : 0u, mhi = lane < 32 ? 0u : 1u << (lane & 31);
@@ -348,6 +492,7 @@ __device__ __forceinline__ uint32_t visible_tree(int P, unsigned long long anc, 
 // Scores of keys that the lane's row does not see become -inf.  A key's place among the lane's scores is a constant once the lane's half is
 // shifted out, so a score takes two instructions.
 __device__ __forceinline__ void hide(f32x16& s, uint32_t visible, int hf) {
+    asm volatile("" : "+v"(visible));          // (stays behind its branch: few tiles need it, and the compiler would do it for all)
     visible >>= 4 * hf;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -356,14 +501,14 @@ __device__ __forceinline__ void hide(f32x16& s, uint32_t visible, int hf) {
     }
 }
 
-// The four key streams of a workgroup meet in LDS, and the result is stored, or joins those of the other ranges of keys.
+// The four key streams of a workgroup meet in LDS, and the result is stored, or joins the item's other parts.
 template <int D, int QB>
 __device__ __forceinline__ void finish(const ChunkParams& p, const Item& it, const Rows<QB>& rows, const f32x16 (&acc)[QB][D / 32], const float (&m_run)[QB],
                                        const float (&l_run)[QB], unsigned char* s_mem, float (*s_m)[QB * 32], float (*s_l)[QB * 32]) {
     constexpr int NT = D / 32, ROWS = QB * 32;
     constexpr int NB = QB * NT;                            // (32 rows, 32 dims) blocks of the result
     constexpr int OWN = NB >= kWaveWgs ? NB / kWaveWgs : 1;
-    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+    const int tid = this_thread(), lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = it.b, hk = it.hk;
     // Block x: rows 32 (x / NT), dims 32 (x % NT); wavefront w owns blocks OWN w .. (head size 64 and 32 rows: the first two have one each).
@@ -425,7 +570,7 @@ __device__ __forceinline__ void finish(const ChunkParams& p, const Item& it, con
             }
         }
     }
-    if (it.c == 1) {
+    if (it.parts == 1) {
         if (wave < NB / OWN) {
 #pragma unroll
             for (int e = 0; e < OWN; ++e) {
@@ -439,14 +584,10 @@ __device__ __forceinline__ void finish(const ChunkParams& p, const Item& it, con
         }
         return;
     }
-    // ---- partial result of this range of keys, and the merge by the last of them -----------------
-    // A partial: [block][4][64 lanes] vectors of four fp32 (the accumulators as they are, rows of the group that exist only), then a (maximum,
-    // sum) pair per row.
-    constexpr int kPartBytes = ROWS * (D + 2) * 4;
-    unsigned char* const parts = p.ws_part + static_cast<int64_t>(it.index - it.x * step_of(p, it, ROWS)) * kPartBytes;
-    const int64_t part_step = static_cast<int64_t>(step_of(p, it, ROWS)) * kPartBytes;
+    // ---- this part of the result, and the merge by the workgroup that comes last -----------------
+    // A part: [block][4][64 lanes] vectors of four fp32 (the accumulators as they are, rows that exist only), then a (maximum, sum) pair per row.
     if (wave < NB / OWN) {
-        unsigned char* const mine = parts + it.x * part_step;
+        unsigned char* const mine = p.ws_part + part_at(it, it.part, part_bytes(ROWS, D));
 #pragma unroll
         for (int e = 0; e < OWN; ++e) {
             const int block = wave * OWN + e, qb = block / NT;
@@ -468,14 +609,14 @@ __device__ __forceinline__ void finish(const ChunkParams& p, const Item& it, con
     if (tid == 0) {
         int32_t* const cnt = p.ws_cnt + ((static_cast<int64_t>(b) * p.H_kv + hk) * p.row_blocks + it.rb) * kCounterStride;
         const int ticket = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const bool last = ticket == it.c - 1;
+        const bool last = ticket == it.parts - 1;
         if (last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         *s_last = last;
     }
     __syncthreads();
     if (!*s_last) return;
     asm volatile("" ::: "memory");
-    merge_ranges<D, ROWS>(p, it, parts, part_step, s_mem);
+    merge_parts<D, ROWS>(p, it, s_mem);
 }
 
 }  // namespace

@@ -13,6 +13,90 @@ namespace specvlm {
 
 namespace {
 
+// A shared block's part of a wavefront's 64 rows joins the other parts.  The last to come has the whole result afterwards, the same whoever that
+// is (the parts are added in their order), and returns true; its own part does not go through memory.
+// A part: [wavefront][2 NT blocks][4][64 lanes] vectors of four fp32, then (maximum, sum) pairs.
+template <int NT>
+__device__ __forceinline__ bool join(const ChunkParams& p, const Item& it, int wave, int lane, float (&M)[2], float (&L)[2], f32x16 (&acc)[2][NT]) {
+    constexpr int kCoherent = 16;                          // device-coherent (sc1) loads, which the compiler counts
+    constexpr int kPart = part_bytes(kSharedRows, 32 * NT), kWave = 2 * NT * 4096;
+    const int l32 = lane & 31, hf = lane >> 5;
+    int32_t* const cnt = p.ws_cnt + ((static_cast<int64_t>(it.b) * p.H_kv + it.hk) * p.row_blocks + it.rb) * kCounterStride + wave;
+    int before = 0;
+    if (lane == 0) before = __hip_atomic_load(cnt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (u(before) != it.parts - 1) {
+        unsigned char* const mine = p.ws_part + part_at(it, it.part, kPart);
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    u32x4 x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(acc[qb][t][4 * v + i]);
+                    store16_coherent(mine + wave * kWave + (((qb * NT + t) * 4 + v) * 64 + lane) * 16, x);
+                }
+            if (hf == 0) store8_coherent(mine + 4 * kWave + (wave * 64 + qb * 32 + l32) * 8, u32x2{__float_as_uint(M[qb]), __float_as_uint(L[qb])});
+        }
+        wait_vmcnt<0>();
+        if (lane == 0) before = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (u(before) != it.parts - 1) return false;
+    }
+    if (lane == 0) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::: "memory");
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(p.ws_part, 0, 0x7FFFFFFF, 0x00027000);
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int ml_off = 4 * kWave + (wave * 64 + qb * 32 + l32) * 8;
+        auto pair = [&](int i) __attribute__((always_inline)) {
+            return __builtin_amdgcn_raw_buffer_load_b64(rsrc, ml_off, static_cast<int>(part_at(it, i, kPart)), kCoherent);
+        };
+        float most = M[qb];
+        for (int i = 0; i < it.parts; ++i)
+            if (i != it.part) most = fmaxf(most, __uint_as_float(pair(i)[0]));
+        const float m_safe = most == -INFINITY ? 0.f : most;
+        const float own = fast_exp2((M[qb] - m_safe) * p.c2);
+        float sum = 0.f;
+        f32x16 out[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) out[t][i] = 0.f;
+        for (int i = 0; i < it.parts; ++i) {
+            if (i == it.part) {
+                sum += L[qb] * own;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) out[t][e] = fmaf(acc[qb][t][e], own, out[t][e]);
+                continue;
+            }
+            const int at = static_cast<int>(part_at(it, i, kPart));
+            const auto ml = pair(i);
+            u32x4 x[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    x[t][v] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, wave * kWave + (((qb * NT + t) * 4 + v) * 64 + lane) * 16, at, kCoherent);
+            const float w = fast_exp2((__uint_as_float(ml[0]) - m_safe) * p.c2);
+            sum += __uint_as_float(ml[1]) * w;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[t][4 * v + e] = fmaf(__uint_as_float(x[t][v][e]), w, out[t][4 * v + e]);
+        }
+        M[qb] = most;
+        L[qb] = sum;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[qb][t] = out[t];
+    }
+    return true;
+}
+
 template <int D, bool E4M3, bool PAGED, bool SHARED>
 __device__ __forceinline__ void attend64(const ChunkParams& p) {
     constexpr int QB = 2;
@@ -35,50 +119,35 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
     __shared__ float s_m[SHARED ? 1 : kWaveWgs][QB * 32];
     __shared__ float s_l[SHARED ? 1 : kWaveWgs][QB * 32];
 
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l32 = lane & 31, hf = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    using W = Work<ChunkParams, SHARED ? kSharedRows : 64, SHARED>;
+    __shared__ std::conditional_t<SHARED, Segments, int> s_segments;
     Item it;
+    for (int turn = 0; ; ++turn) {
     if constexpr (SHARED) {
-        // the blocks with the most keys first; the blocks of a head on one XCD where the number of heads allows it
-        typedef const __attribute__((address_space(4))) int32_t* const_i32;
-        const uint32_t pairs = static_cast<uint32_t>(p.B) * p.H_kv;
-        const uint32_t level = blockIdx.x / pairs, pair = blockIdx.x - level * pairs;
-        it.rb = p.row_blocks - 1 - level;
-        it.b = pair / static_cast<uint32_t>(p.H_kv);
-        it.hk = pair - it.b * p.H_kv;
-        it.x = 0;
-        it.c = 1;
-        it.n = p.num_new ? ((const_i32)p.num_new)[it.b] : p.N_max;
-        it.P = ((const_i32)p.prefix_len)[it.b];
-        if (const int err = length_error(p, it.n, it.P)) {
-            if (it.rb == 0 && it.hk == 0 && tid == 0 && p.err_flag) atomicOr(p.err_flag, err);
-            return;
-        }
-        if (it.rb * kSharedRows >= p.group * it.n) return;
+        if (!next_segment<kSharedRows, true>(p, s_segments, turn, it)) return;
     } else {
-        if (!find_item<64>(p, lane, it)) return;
+        if (turn || !find_item<64, 3, 4>(p, threadIdx.x & 63, it)) return;
         it = uniform(it);
     }
+    const int lane = this_thread() & 63, l32 = lane & 31, hf = lane >> 5;
     const int b = it.b, hk = it.hk, n = it.n, P = it.P, S = P + n;
     const int row0 = it.rb * (SHARED ? kSharedRows : 64) + (SHARED ? wave * 64 : 0);       // of the wavefront
-    const Rows<QB> rows(p, hk, n, row0);
+    const Rows<QB> rows(p, hk, n, row0, l32);
     unsigned long long anc[QB] = {};
     if constexpr (!SHARED) {
-        if (p.parent && !ancestors(p, it, lane, rows.token, anc)) return;
+        if (p.parent && !ancestors(p, it, lane, rows.token, anc)) continue;
     }
     const bool tree = !SHARED && p.parent;
     const int first_token = min(static_cast<int>(divide(row0, p.magic_group)), n - 1);
-    const int last_token = min(static_cast<int>(divide((it.rb + 1) * (SHARED ? kSharedRows : 64) - 1, p.magic_group)), n - 1);
+    const int last_token = W::last_token(p, n, it.rb);
     const int all_see = tree ? P : P + first_token + 1;    // slots that every row of the wavefront sees
     const int end = tree ? S : P + last_token + 1;         // slots that some row of the workgroup sees
-    // Tiles: all of them (shared), or those of this range of keys and this stream: whole rounds of the request, up to the block's end.
-    int tile0 = 0, ntile = (end - 1) / kKeys + 1;          // first; number
+    // Tiles of this segment: first; number.  Streams: up to the block's end, this wavefront's has every fourth.
+    int tile0 = it.from, ntile = it.to - it.from;
     if constexpr (!SHARED) {
-        const int rounds = static_cast<int>((static_cast<uint32_t>(S - 1) + kSharesRound) / kSharesRound);
-        const int first_round = it.x * rounds / it.c, next_round = (it.x + 1) * rounds / it.c;
-        tile0 = first_round * kWaveWgs + wave;
-        const int past = min(ntile, next_round * kWaveWgs);
+        tile0 = it.from * kWaveWgs + wave;
+        const int past = min((end - 1) / kKeys + 1, it.to * kWaveWgs);
         ntile = tile0 < past ? (past - tile0 + kWaveWgs - 1) / kWaveWgs : 0;
     }
 
@@ -97,7 +166,7 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
     constexpr int kIdTiles = SHARED ? 64 : 32;
     int ids = 0, ids_next = 0;
     auto request_ids = [&](int tile) __attribute__((always_inline)) {
-        const int blk = SHARED ? (tile + lane) * 2 + half : (tile0 + (tile + (lane >> 1)) * STEP) * 2 + (lane & 1);
+        const int blk = SHARED ? (tile0 + tile + lane) * 2 + half : (tile0 + (tile + (lane >> 1)) * STEP) * 2 + (lane & 1);
         return p.g.block_table[static_cast<int64_t>(b) * p.g.max_blocks + min(blk, last_blk)];
     };
     auto take_ids = [&](int raw) __attribute__((always_inline)) {
@@ -285,7 +354,6 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
         for (int i = 0; i < decltype(products)::value; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // a matrix product
             __builtin_amdgcn_sched_group_barrier(0x402, 4, 0);      // and vector instructions in its shadow
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
     };
     auto pin = [&](int qb) __attribute__((always_inline)) {          // (the weights are computed here, not behind a branch where they are used)
@@ -454,18 +522,25 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
     }
     if (PAGED && __any(bad_block) && lane == 0 && p.err_flag) atomicOr(p.err_flag, SPECVLM_ERR_BAD_BLOCK);
     if constexpr (SHARED) {
+        float M[QB], L[QB];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-            const float L = l_run[qb] + other_half(l_run[qb]);
-            const float inv = 1.f / L;
+            M[qb] = m_run[qb];
+            L[qb] = l_run[qb] + other_half(l_run[qb]);
+        }
+        if (it.parts > 1 && !join(p, it, wave, lane, M, L, acc)) continue;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const float inv = 1.f / L[qb];
             uint16_t* const row = p.o + b * p.o_sb + rows.token[qb] * p.o_sn + rows.head[qb] * p.o_sh + 8 * hf;
 #pragma unroll
             for (int t = 0; t < NT; ++t) store_block(acc[qb][t], inv, row + 32 * t, rows.real[qb]);
             if (rows.real[qb] && p.lse && hf == 0)
-                p.lse[(static_cast<int64_t>(b) * p.H_q + rows.head[qb]) * p.N_max + rows.token[qb]] = m_run[qb] * p.scale + __log2f(L) * kLn2;
+                p.lse[(static_cast<int64_t>(b) * p.H_q + rows.head[qb]) * p.N_max + rows.token[qb]] = M[qb] * p.scale + __log2f(L[qb]) * kLn2;
         }
     } else {
         finish<D, QB>(p, it, rows, acc, m_run, l_run, s_mem, s_m, s_l);
+    }
     }
 }
 

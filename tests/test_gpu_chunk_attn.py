@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from chunk_util import Cache, check_attention, gen, i32, random_tree
+from chunk_util import Cache, attention64, check_attention, gen, i32, random_tree
 
 pytestmark = pytest.mark.gpu
 BF16, E4M3 = torch.bfloat16, torch.float8_e4m3fn
@@ -87,10 +87,12 @@ def test_a_chunk_is_its_tokens_one_at_a_time(sv):
     cache = Cache(g, [P + N], 2, 128, E4M3, True)
     q = queries(g, 1, N, 8, 128)
     whole = sv.specvlm_chunk_attn(q, cache.k, cache.v, i32([P]), block_table=cache.table, scales=cache.scales)
+    bound = attention64(q, cache, 0, P, N)[2]
     for i in range(N):
         one = sv.specvlm_chunk_attn(q[:, i:i + 1].contiguous(), cache.k, cache.v, i32([P + i]), block_table=cache.table, scales=cache.scales)
-        d = (whole[0, i].float() - one[0, 0].float()).abs().max()
-        assert d <= 2.0 ** -6                    # two roundings of weights and results each, of values up to 1
+        # each of the two is off by no more than its bound from the exact result, which is the same; results are not bounded by 1 (e4m3 rows here
+        # have scales up to e^2 or so), and half a bf16 step of 4 .. 8 alone is 2^-6
+        assert bool(((whole[0, i].double() - one[0, 0].double()).abs() <= 2 * bound[i]).all())
 
 
 def test_chain_tree_is_causal(sv):

@@ -87,7 +87,7 @@ __device__ __forceinline__ void attend32(const ChunkParams& p) {
                 sbase += slot0;
                 row = min(i * RPI + lrow, S - 1 - slot0);
             }
-            raw.w[i] = *reinterpret_cast<const u32x4*>(base + (row * row_bytes + lpos * 16));
+            raw.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + (row * row_bytes + lpos * 16)));
             if constexpr (E4M3) raw.e[i] = sbase[row];
         }
     };
@@ -150,26 +150,35 @@ __device__ __forceinline__ void attend32(const ChunkParams& p) {
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[0][t] = zero;
-    Raw kraw, vraw;
+    // Tiles on their way through registers: one, of e4m3 caches two (tile j in set j % 2)
+    constexpr int SETS = E4M3 ? 2 : 1;
+    Raw kraw[SETS], vraw[SETS];
+    auto bring = [&](int set, int tile) __attribute__((always_inline)) {
+        if (tile >= my_tiles) return;
+        if (PAGED && tile && (tile & 31) == 0) {
+            take_ids(ids_next);
+            if (tile + 32 < my_tiles) ids_next = request_ids(tile + 32);
+        }
+        load(kraw[set], p.k, p.ks, tile);
+        load(vraw[set], p.v, p.vs, tile);
+    };
     if (my_tiles > 0) {
         if constexpr (PAGED) {
             take_ids(request_ids(0));
             if (my_tiles > 32) ids_next = request_ids(32);
         }
-        load(kraw, p.k, p.ks, 0);
-        load(vraw, p.v, p.vs, 0);
+        bring(0, 0);
+        if constexpr (SETS == 2) bring(1, 1);
         const uint16_t* row = p.q + b * p.q_sb + rows.token[0] * p.q_sn + rows.head[0] * p.q_sh + 8 * hf;
 #pragma unroll
         for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const bf16x8*>(row + 16 * c);
-        store(kraw, std::false_type{});
-        store(vraw, std::true_type{});
-        if (my_tiles > 1) {
-            load(kraw, p.k, p.ks, 1);
-            load(vraw, p.v, p.vs, 1);
-        }
+        store(kraw[0], std::false_type{});
+        store(vraw[0], std::true_type{});
+        bring(0, SETS);
         wave_order();
     }
-    for (int j = 0; j < my_tiles; ++j) {
+    auto step = [&](auto next_set, int j) __attribute__((always_inline)) {
+        constexpr int NEXT_SET = decltype(next_set)::value;
         const int slot0 = (tile0 + j * kWaveWgs) * kKeys;
         read_k();
         f32x16 s;
@@ -211,18 +220,19 @@ __device__ __forceinline__ void attend32(const ChunkParams& p) {
         }
         wave_order();
         if (j + 1 < my_tiles) {
-            store(kraw, std::false_type{});
-            store(vraw, std::true_type{});
-            if (j + 2 < my_tiles) {
-                if (PAGED && ((j + 2) & 31) == 0) {
-                    take_ids(ids_next);
-                    if (j + 2 + 32 < my_tiles) ids_next = request_ids(j + 2 + 32);
-                }
-                load(kraw, p.k, p.ks, j + 2);
-                load(vraw, p.v, p.vs, j + 2);
-            }
+            store(kraw[NEXT_SET], std::false_type{});
+            store(vraw[NEXT_SET], std::true_type{});
+            bring(NEXT_SET, j + 1 + SETS);
             wave_order();
         }
+    };
+    if constexpr (SETS == 2) {
+        for (int j = 0; j < my_tiles; j += 2) {
+            step(std::integral_constant<int, 1>{}, j);
+            if (j + 1 < my_tiles) step(std::integral_constant<int, 0>{}, j + 1);
+        }
+    } else {
+        for (int j = 0; j < my_tiles; ++j) step(std::integral_constant<int, 0>{}, j);
     }
     if (PAGED && __any(bad_block) && lane == 0 && p.err_flag) atomicOr(p.err_flag, SPECVLM_ERR_BAD_BLOCK);
     finish<D, 1>(p, it, rows, acc, m_run, l_run, s_mem, s_m, s_l);

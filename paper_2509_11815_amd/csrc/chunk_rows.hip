@@ -107,10 +107,10 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
     constexpr int STEP = SHARED ? 1 : kWaveWgs;    // tiles from one of a stream to its next
     constexpr int kTileBytes = kKeys * ROWB;
     // Tiles of K, and of V, in LDS, and how many tiles before a tile's weights its K and V are asked for (e4m3: from memory into registers two
-    // tiles (shared) or one before that).
+    // tiles before that).
     constexpr int SLOTS = SHARED ? (E4M3 ? 2 : 4) : (E4M3 ? 1 : 2);
     constexpr int K_LEAD = E4M3 ? 2 : SHARED ? 4 : 3, V_LEAD = K_LEAD - 1;
-    constexpr int SETS = E4M3 ? (SHARED ? 2 : 1) : 0;
+    constexpr int SETS = E4M3 ? 2 : 0;
     constexpr int kAreaBytes = 2 * SLOTS * kTileBytes;     // of a stream
     constexpr int kMergeBytes = SHARED ? 0 : QB * NT * 3 * 4096;
     constexpr int kTiles = (SHARED ? 1 : kWaveWgs) * kAreaBytes;
@@ -340,6 +340,7 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
         if constexpr (SHARED) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         else asm volatile("" ::: "memory");
     };
+    // e4m3: set x of K holds tiles x (mod 2) and of V tiles x + 1 (mod 2); shared: what the wavefront brings, in raw_k
     Raw raw_k[SETS ? SETS : 1], raw_v[SETS && !SHARED ? SETS : 1];
     auto request_q = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -376,10 +377,10 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
             load(raw_k[SET], is_v, j + (is_v ? V_LEAD : K_LEAD) + 2);
         } else {
             asm volatile("" ::: "memory");
-            store(raw_v[0], true, j + V_LEAD);
-            load(raw_v[0], true, j + V_LEAD + 1);          // (before the ids change)
-            store(raw_k[0], false, j + K_LEAD);
-            load(raw_k[0], false, j + K_LEAD + 1);
+            store(raw_v[SET], true, j + V_LEAD);
+            load(raw_v[SET], true, j + V_LEAD + 2);        // (before the ids change)
+            store(raw_k[SET], false, j + K_LEAD);
+            load(raw_k[SET], false, j + K_LEAD + 2);
         }
     };
     auto land = [&](int j) __attribute__((always_inline)) {
@@ -468,12 +469,14 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
             }
         } else {
             load(raw_k[0], false, 0);
-            load(raw_v[0], true, 0);
+            load(raw_v[1], true, 0);
+            load(raw_k[1], false, 1);
+            load(raw_v[0], true, 1);
             request_q();
             store(raw_k[0], false, 0);
-            load(raw_k[0], false, 1);
-            store(raw_v[0], true, 0);
-            load(raw_v[0], true, 1);
+            load(raw_k[0], false, 2);
+            store(raw_v[1], true, 0);
+            load(raw_v[1], true, 2);
         }
         meet();
         read_k(0);
@@ -482,8 +485,8 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
             meet();
         } else if constexpr (E4M3) {
             meet();
-            store(raw_k[0], false, 1);
-            load(raw_k[0], false, 2);
+            store(raw_k[1], false, 1);
+            load(raw_k[1], false, 3);
             meet();
         } else {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

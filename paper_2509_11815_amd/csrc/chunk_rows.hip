@@ -127,7 +127,7 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
     if constexpr (SHARED) {
         if (!next_segment<kSharedRows, true>(p, s_segments, turn, it)) return;
     } else {
-        if (turn || !find_item<64, 3, 4>(p, threadIdx.x & 63, it)) return;
+        if (turn || !find_item<64, 3, 14>(p, threadIdx.x & 63, it)) return;
         it = uniform(it);
     }
     const int lane = this_thread() & 63, l32 = lane & 31, hf = lane >> 5;

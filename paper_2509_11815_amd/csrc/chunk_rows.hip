@@ -202,7 +202,9 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
         return at;
     };
     auto vswz = [](int r) { return D == 128 ? (r & 3) : ((r >> 1) & 1); };
-    // K row r in LDS: granule g at g ^ (r % ROWG); V row r: 64-byte chunk c at c ^ vswz(r), so that the operand reads meet no bank twice
+    // (e4m3 streams: the rows of a store lie KI apart, so that their lowest bits go last)
+    auto kswz = [](int r) { return E4M3 && !SHARED ? (r & (ROWG - 1)) / KI | (r & (KI - 1)) * (ROWG / KI) : r & (ROWG - 1); };
+    // K row r in LDS: granule g at g ^ kswz(r); V row r: 64-byte chunk c at c ^ vswz(r), so that the operand reads meet no bank twice
     typedef __attribute__((address_space(3))) unsigned char lds_byte;
     unsigned char* const area = s_mem + (SHARED ? 0 : wave * kAreaBytes);
     constexpr int kVArea = SLOTS * kTileBytes;
@@ -223,26 +225,51 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
             }
         }
     };
-    // e4m3: through registers, where codes become bf16 (exact; the row's scale goes into the conversion)
-    struct Raw { u32x4 w[KI]; uint32_t e[KI]; };
+    // e4m3: through registers, where codes become bf16 (exact; the row's scale goes into the conversion).  Streams: a lane has KI rows beside one
+    // another and their scales in one load, for a byte a lane takes the address unit as long as sixteen (four trees over 4864 slots 66.8 -> 64.3 us);
+    // shared, where a wavefront brings a quarter as much, a row of every load instruction (1024, 1024 and 333 tokens 252 us, beside one another 276).
+    constexpr bool BESIDE = !SHARED;
+    struct Raw { u32x4 w[KI]; uint32_t e[BESIDE ? 1 : KI]; };
+    const int my_row = BESIDE ? lrow * KI : lrow;
+    const uint32_t my_off = (my_row & 15) * row_bytes + lpos * 16;
     auto load = [&](Raw& raw, bool v, int tile) __attribute__((always_inline)) {
         if (tile >= ntile) return;
         if (SHARED || !v) ids_for(tile);
+        const unsigned char *const cache = v ? p.v : p.k, *const scales = v ? p.vs : p.ks;
+        const Half low = half_of(cache, scales, tile, 0);
+        if constexpr (!BESIDE) {
 #pragma unroll
-        for (int i = 0; i < KI; ++i) {
-            const Half at = half_of(v ? p.v : p.k, v ? p.vs : p.ks, tile, i * RPI / 16);
-            const uint32_t row = min(i * RPI % 16 + lrow, at.last);
-            raw.w[i] = *reinterpret_cast<const u32x4*>(at.base + (row * row_bytes + lpos * 16));
-            raw.e[i] = at.sbase[row];
+            for (int i = 0; i < KI; ++i) {
+                const uint32_t row = min(i * RPI + lrow, low.last);
+                raw.w[i] = *reinterpret_cast<const u32x4*>(low.base + (row * row_bytes + lpos * 16));
+                raw.e[i] = low.sbase[row];
+            }
+        } else {
+            const Half high = half_of(cache, scales, tile, 1), at = hf ? high : low;
+            if (__builtin_expect((tile0 + tile * STEP + 1) * kKeys <= S, 1)) {
+#pragma unroll
+                for (int i = 0; i < KI; ++i) raw.w[i] = *reinterpret_cast<const u32x4*>(at.base + static_cast<uint64_t>(i * row_bytes) + my_off);
+                std::conditional_t<KI == 4, uint32_t, uint16_t> e;
+                __builtin_memcpy(&e, at.sbase + (my_row & 15), KI);
+                raw.e[0] = e;
+            } else {
+                raw.e[0] = 0;
+#pragma unroll
+                for (int i = 0; i < KI; ++i) {
+                    const uint32_t row = min((my_row & 15) + i, at.last);
+                    raw.w[i] = *reinterpret_cast<const u32x4*>(at.base + (row * row_bytes + lpos * 16));
+                    raw.e[0] |= static_cast<uint32_t>(at.sbase[row]) << (8 * i);
+                }
+            }
         }
     };
     auto store = [&](const Raw& raw, bool v, int tile) __attribute__((always_inline)) {
         unsigned char* const at = area + (v ? kVArea : 0) + (tile & (SLOTS - 1)) * kTileBytes;
 #pragma unroll
         for (int i = 0; i < KI; ++i) {
-            const int r = half * 16 + i * RPI + lrow;
-            const int swz = v ? vswz(r) << 2 : r & (ROWG - 1);
-            const float scale = __uint_as_float(raw.e[i] << 23);
+            const int r = half * 16 + my_row + (BESIDE ? i : i * RPI);
+            const int swz = v ? vswz(r) << 2 : kswz(r);
+            const float scale = __uint_as_float(!BESIDE ? raw.e[i] << 23 : (i < 3 ? raw.e[0] << (23 - 8 * i) : raw.e[0] >> 1) & 0x7F800000u);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 u32x4 w;
@@ -259,7 +286,7 @@ __device__ __forceinline__ void attend64(const ChunkParams& p) {
     // ---- operands ---------------------------------------------------------------------------
     uint32_t kaddr[NC];                        // lane (key l32, half hf): dims 16c + 8hf .. +7; the query rows likewise
 #pragma unroll
-    for (int c = 0; c < NC; ++c) kaddr[c] = l32 * ROWB + (((2 * c + hf) ^ (l32 & (ROWG - 1))) << 4);
+    for (int c = 0; c < NC; ++c) kaddr[c] = l32 * ROWB + (((2 * c + hf) ^ kswz(l32)) << 4);
     // va[t][x] element e is key 16x + 8 (e / 4) + 4 hf + e % 4, dim 32t + l32 (attn_streams.hip has the same reads)
     const int k0 = 4 * hf + ((lane & 15) >> 2);
     const uint32_t vaddr = k0 * ROWB + ((lane >> 4) & 1) * 32 + (lane & 3) * 8 + (vswz(k0) << 6);

@@ -1,0 +1,410 @@
+"""The cache calls and the attention of token chunks as they are used: together, captured, on other streams, with shared or small workspaces, over
+caches laid out in other orders and too large for 32-bit offsets."""
+import math
+
+import pytest
+import torch
+
+from chunk_util import PAGE, Cache, as_bytes, attention64, check_attention, gen, i32, quantise64, random_tree, two_to
+
+pytestmark = pytest.mark.gpu
+BF16, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def sv():
+    import paper_2509_11815_amd as sv
+    sv.load_library()
+    return sv
+
+
+def normal(g, *shape, dtype=BF16):
+    return torch.empty(shape, dtype=dtype, device="cuda").normal_(generator=g)
+
+
+KINDS = [(BF16, False), (BF16, True), (E4M3, False), (E4M3, True)]
+kinds = pytest.mark.parametrize("dtype,paged", KINDS, ids=["bf16", "bf16-paged", "e4m3", "e4m3-paged"])
+
+
+# ---- a request from its prompt to its second step ----------------------------------------------
+
+class Tokens:
+    """The rows that a request's slots should hold, in 64 bits: the reference's own memory of what was written where."""
+
+    def __init__(self, B, heads, dim, kind):
+        self.rows, self.kind = [[] for _ in range(B)], kind
+
+    def write(self, b, at, k, v):
+        """[n, heads, D] rows at slots at .."""
+        del self.rows[b][at:]
+        for pair in zip(k, v):
+            self.rows[b].append(tuple(self.value(x) for x in pair))
+
+    def value(self, x):
+        if self.kind != E4M3:
+            return x.double()
+        code, e = quantise64(x)
+        return code * two_to(e)[..., None]
+
+    def get(self, b, which):
+        return torch.stack([r[which] for r in self.rows[b]])
+
+
+class View:
+    """Tokens as attention64 reads a cache."""
+
+    def __init__(self, tokens, heads):
+        self.tokens, self.heads = tokens, heads
+
+    def rows64(self, b, slots, which):
+        return self.tokens.get(b, which)[list(slots)]
+
+
+def accepted_depth(parent, tok, amax):
+    """Depth of every node whose token and whose ancestors' tokens are their parents' arg-max; -1: not accepted."""
+    depth = [0]
+    for j in range(1, len(parent)):
+        p = parent[j]
+        depth.append(depth[p] + 1 if depth[p] >= 0 and tok[j] == amax[p] else -1)
+    return depth
+
+
+@kinds
+def test_prompt_tree_acceptance_compaction_and_decoding(sv, dtype, paged):
+    """Chunks of the prompt, a draft tree, arg-max and acceptance, compaction, the next token, the cache read back: every step's rows against a
+    reference that keeps its own tokens."""
+    g = gen(77)
+    B, H, G, D, V = 3, 8, 2, 128, 500
+    lengths, N, room = [61, 130, 5], 20, 60
+    cache = Cache(g, [n + room for n in lengths], G, D, dtype, paged, layers=1)
+    k1, v1 = cache.k[0], cache.v[0]
+    scales = None if cache.ks is None else (cache.ks[0], cache.vs[0])
+    kw = dict(block_table=cache.table, scales=scales)
+    tokens, err = Tokens(B, G, D, dtype), i32([0])
+    workspace = torch.zeros(sv.CHUNK_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+
+    def step(prefix, new, parent=None):
+        """One pass of the layer over new tokens: their rows into the cache, attention over it."""
+        width = max(new)
+        fused = normal(g, B, width, H + 2 * G, D)
+        q, k, v = fused[:, :, :H], fused[:, :, H:H + G], fused[:, :, H + G:]
+        P, n = i32(prefix), i32(new)
+        sv.specvlm_kv_append(k, v, k1, v1, P, num_new=n, err_flag=err, **kw)
+        out = sv.specvlm_chunk_attn(q, k1, v1, P, num_new=n, parent=parent, workspace=workspace, err_flag=err, **kw)
+        for b in range(B):
+            tokens.write(b, prefix[b], k[b, :new[b]], v[b, :new[b]])
+            if new[b]:
+                o, _, tol, _ = attention64(q, View(tokens, G), b, prefix[b], new[b], parent)
+                assert bool(((out[b, :new[b]].double() - o).abs() <= tol).all()), (b, prefix, new)
+        return out
+
+    done = [0] * B
+    while any(d < n for d, n in zip(done, lengths)):       # the prompt, 48 tokens at a time
+        new = [min(48, n - d) for d, n in zip(done, lengths)]
+        step(done, new)
+        done = [d + n for d, n in zip(done, new)]
+    for _ in range(2):                                     # two verification steps
+        parent = torch.stack([random_tree(g, N) for _ in range(B)])
+        nodes = [N, N - 7, 1]
+        hidden = step(done, nodes, parent)
+        logits = (hidden.reshape(B, N, H * D).float() @ normal(g, H * D, V, dtype=F32)).to(BF16)
+        amax = sv.specvlm_node_argmax(logits, num_nodes=i32(nodes))
+        # (about every second node's draft token is what its parent would say)
+        right = torch.gather(amax, 1, parent.clamp(min=0).long())
+        draft = torch.where(torch.rand((B, N), generator=g, device="cuda") < 0.6, right, (right + 1) % V).to(torch.int32)
+        length, path, bonus, _ = sv.specvlm_tree_accept(parent, draft, amax, num_nodes=i32(nodes), path_cap=8, err_flag=err)
+        P = i32(done)
+        if dtype == E4M3:
+            sv.specvlm_kv_compact_quantized(cache.k, cache.v, cache.scales, P, path, length, block_table=cache.table, new_prefix_len=P, err_flag=err)
+        else:
+            sv.specvlm_kv_compact(cache.k, cache.v, P, path, length, block_table=cache.table, new_prefix_len=P, err_flag=err)
+        for b in range(B):
+            par, m = parent[b, :nodes[b]].tolist(), int(length[b])
+            depth = accepted_depth(par, draft[b].tolist(), amax[b].tolist())
+            want = path[b, :m + 1].tolist()
+            assert want[0] == 0 and all(par[j] == i for i, j in zip(want, want[1:])) and m == min(7, max(depth)) and depth[want[-1]] == m
+            kept = [tokens.rows[b][done[b] + j] for j in want]
+            tokens.rows[b][done[b]:] = kept
+            done[b] += m + 1
+        assert P.tolist() == done
+    step(done, [1, 0, 1])                                  # one more token, the second request waits
+    done = [done[0] + 1, done[1], done[2] + 1]
+    k, v = sv.specvlm_kv_read(k1, v1, i32(done), max(done), err_flag=err, **kw)
+    for b in range(B):
+        for which, x in enumerate((k, v)):
+            assert torch.equal(x[b, :done[b]].double(), tokens.get(b, which))
+            assert bool((x[b, done[b]:] == 0).all())
+    assert int(err) == 0
+
+
+# ---- graphs, streams, workspaces ----------------------------------------------------------------
+
+@kinds
+@pytest.mark.parametrize("N,H,G,prefix", [(1, 16, 4, [3000, 40, 900]), (60, 8, 8, [1000, 33, 2000]), (200, 8, 2, [500, 0, 1500]), (700, 8, 8, [0, 77, 300])])
+def test_captured_and_replayed(sv, dtype, paged, N, H, G, prefix):
+    """Append and attention in a graph, replayed over changing lengths and rows with eager calls of the same workspace between."""
+    g = gen(N)
+    B, D = 3, 128
+    tree = N == 60
+    cache = Cache(g, [p + 2 * N + 3 for p in prefix], G, D, dtype, paged)
+    q, k, v = normal(g, B, N, H, D), normal(g, B, N, G, D), normal(g, B, N, G, D)
+    P, n, err = i32(prefix), i32([N] * B), i32([0])
+    parent = torch.stack([random_tree(g, N) for _ in range(B)]) if tree else None
+    out, lse = torch.zeros_like(q), torch.zeros((B, H, N), device="cuda")
+    ws = torch.zeros(sv.CHUNK_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+
+    def both(out, lse):
+        sv.specvlm_kv_append(k, v, cache.k, cache.v, P, num_new=n, block_table=cache.table, scales=cache.scales, err_flag=err)
+        sv.specvlm_chunk_attn(q, cache.k, cache.v, P, num_new=n, parent=parent, block_table=cache.table, scales=cache.scales, out=out, lse=lse,
+                              workspace=ws, err_flag=err)
+
+    both(out, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(out, lse)
+    for turn in range(4):
+        P.copy_(i32([p + turn * (N // 3 + 1) for p in prefix]))
+        n.copy_(i32([N, max(1, N - turn), 0 if turn == 2 else N]))
+        for t in (q, k, v):
+            t.normal_(generator=g)
+        out.fill_(3.0)
+        lse.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        out.fill_(3.0)
+        lse.fill_(3.0)
+        both(out, lse)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out) and torch.equal(got[1], lse), turn
+        for b in range(B):
+            m = int(n[b])
+            assert bool((out[b, m:] == 3.0).all())
+            if m and (b == turn % B):
+                o, _, tol, _ = attention64(q, cache, b, int(P[b]), m, parent)
+                assert bool(((out[b, :m].double() - o).abs() <= tol).all()), (turn, b)
+    assert int(err) == 0 and not bool(ws[:512 << 10].any())
+
+
+@kinds
+def test_other_streams(sv, dtype, paged):
+    """On a stream of the caller's, with everything omitted that may be, and on the current one when that is not the default."""
+    g = gen(3)
+    cache = Cache(g, [2000, 300], 2, 128, dtype, paged)
+    q = normal(g, 2, 9, 8, 128)
+    P, count, start = i32([1991, 291]), i32([2000, 300]), i32([0, 0])      # (live as long as any stream uses them)
+    want = sv.specvlm_chunk_attn(q, cache.k, cache.v, P, block_table=cache.table, scales=cache.scales)
+    k, v = sv.specvlm_kv_read(cache.k, cache.v, count, 2000, block_table=cache.table, scales=cache.scales)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    busy = normal(g, 4096, 4096)
+    for explicit in (True, False):
+        with torch.cuda.stream(stream):
+            late = torch.zeros_like(q)
+            for _ in range(20):
+                busy @ busy
+            late.copy_(q)                                  # (behind the products: a call on another stream would read zeros)
+        kw = dict(block_table=cache.table, scales=cache.scales)
+        if explicit:
+            got = sv.specvlm_chunk_attn(late, cache.k, cache.v, P, stream=stream, **kw)
+            k2, v2 = sv.specvlm_kv_read(cache.k, cache.v, count, 2000, stream=stream, **kw)
+            sv.specvlm_kv_append(k2, v2, cache.k, cache.v, start, num_new=count, stream=stream, **kw)
+        else:
+            with torch.cuda.stream(stream):
+                got = sv.specvlm_chunk_attn(late, cache.k, cache.v, P, **kw)
+                k2, v2 = sv.specvlm_kv_read(cache.k, cache.v, count, 2000, **kw)
+        stream.synchronize()
+        assert torch.equal(got, want) and torch.equal(k2, k) and torch.equal(v2, v)
+    torch.cuda.synchronize()
+    for b, n in enumerate((2000, 300)):                    # what was read and written back is what was there
+        for which, x in enumerate((k, v)):                 # (values: a row whose greatest number was rounded down may get the next smaller scale)
+            assert torch.equal(cache.rows64(b, range(n), which), x[b, :n].double())
+
+
+@kinds
+def test_workspaces(sv, dtype, paged):
+    """The same results within their bounds with a workspace that is too small, none, or division forbidden; the same bits with one that other
+    shapes have used; counters are zero after every call."""
+    g = gen(12)
+    shapes = [(1, 8, 2, [5000], [1]), (1, 32, 8, [3000] * 4, [1, 0, 1, 1]), (33, 8, 2, [2000, 5], [33, 2]), (257, 4, 4, [1300], [257]),
+              (1200, 8, 8, [0], [1200]), (300, 16, 2, [2000, 100], [300, 299])]
+    ws = torch.zeros(sv.CHUNK_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    made = []
+    for N, H, G, prefix, new in shapes:
+        cache = Cache(g, [p + n for p, n in zip(prefix, new)], G, 128, dtype, paged)
+        q = normal(g, len(prefix), N, H, 128)
+        first, _ = check_attention(sv, q, cache, prefix, new, workspace=ws)
+        assert not bool(ws[:512 << 10].any())
+        made.append((cache, q, prefix, new, first))
+    empty = torch.zeros(0, dtype=torch.uint8, device="cuda")
+    for cache, q, prefix, new, first in reversed(made):
+        again, _ = check_attention(sv, q, cache, prefix, new, workspace=ws)
+        assert torch.equal(again, first)                   # (what the workspace held does not matter, nor which workgroup comes last)
+        fresh, _ = check_attention(sv, q, cache, prefix, new)
+        # (a call without one is given one of the size it asks for; that the results are the same says that it asks for enough)
+        assert torch.equal(fresh, first)
+        check_attention(sv, q, cache, prefix, new, num_splits=1, workspace=empty)
+        check_attention(sv, q, cache, prefix, new, num_splits=1)
+        for size in (256, 512 << 10, (512 << 10) + 40 * 33280 + 256, 2 << 20, 5 << 20):
+            small = torch.zeros(size + 64, dtype=torch.uint8, device="cuda")
+            small[size:] = 0xA5                            # behind its end nothing is written
+            check_attention(sv, q, cache, prefix, new, workspace=small[:size])
+            assert bool((small[size:] == 0xA5).all()) and not bool(small[:min(size, 512 << 10)].any())
+
+
+# ---- layouts ------------------------------------------------------------------------------------
+
+def relaid(cache, order):
+    """The cache's tensors with their (request or block, head, slot) dimensions in another order in memory, gaps between rows and heads."""
+    def lay(t, scale):
+        dims = [0, 1, 2]
+        big = list(t.shape[:3])
+        where = order if not scale else [d for d in order if d != 2] + [2]         # (a head's scales are adjacent)
+        pad = [big[d] + (3 if d == where[1] else 0) for d in where]
+        tail = [] if scale else [t.shape[3] + 16]
+        base = torch.full(pad + tail, 255 if scale or t.element_size() == 1 else 0, dtype=torch.uint8 if t.element_size() == 1 else t.dtype, device="cuda")
+        if t.element_size() != 1:
+            base.fill_(math.nan)
+        view = base.permute([where.index(d) for d in dims] + ([] if scale else [3]))
+        view = view[:big[0], :big[1], :big[2]] if scale else view[:big[0], :big[1], :big[2], :t.shape[3]]
+        view.copy_(as_bytes(t))
+        return view.view(t.dtype) if not scale and t.dtype == E4M3 else view
+    cache.k, cache.v = lay(cache.k, False), lay(cache.v, False)
+    if cache.ks is not None:
+        cache.ks, cache.vs = lay(cache.ks, True), lay(cache.vs, True)
+
+
+@kinds
+@pytest.mark.parametrize("order", [[0, 2, 1], [1, 0, 2], [2, 0, 1], [1, 2, 0]])
+@pytest.mark.parametrize("D", [64, 128])
+def test_cache_orders(sv, dtype, paged, order, D):
+    """Slots outside heads, heads outside requests, slots outermost; rows with gaps."""
+    g = gen(sum(10 ** i * d for i, d in enumerate(order)))
+    for N, prefix, new in ((1, [700, 33], [1, 1]), (70, [100, 7], [70, 33]), (300, [10, 400], [300, 1])):
+        cache = Cache(g, [p + n for p, n in zip(prefix, new)], 3, D, dtype, paged)
+        relaid(cache, order)
+        k, v = normal(g, 2, N, 3, D), normal(g, 2, N, 3, D)
+        sv.specvlm_kv_append(k, v, cache.k, cache.v, i32(prefix), num_new=i32(new), block_table=cache.table, scales=cache.scales)
+        for b, (P, n) in enumerate(zip(prefix, new)):
+            for which, x in enumerate((k, v)):
+                want = x[b, :n].double() if dtype == BF16 else (lambda c, e: c * two_to(e)[..., None])(*quantise64(x[b, :n]))
+                assert torch.equal(cache.rows64(b, range(P, P + n), which), want)
+        check_attention(sv, normal(g, 2, N, 6, D), cache, prefix, new)
+        got = sv.specvlm_kv_read(cache.k, cache.v, i32([p + n for p, n in zip(prefix, new)]), max(prefix) + N, block_table=cache.table, scales=cache.scales)
+        for b, (P, n) in enumerate(zip(prefix, new)):
+            for which, x in enumerate(got):
+                assert torch.equal(x[b, :P + n].double(), cache.rows64(b, range(P + n), which))
+
+
+@kinds
+@pytest.mark.parametrize("N,tree", [(1, False), (40, True), (150, False)])
+def test_offsets_past_32_bits(sv, dtype, paged, N, tree):
+    """Slots, blocks and heads that lie more than 2^32 bytes into the cache."""
+    g = gen(N)
+    D, G, H, P = 64, 2, 2, 340
+    S = P + N
+    size = 1 if dtype == E4M3 else 2
+    heap = torch.zeros(6 << 30, dtype=torch.uint8, device="cuda")
+    cells = heap.view(E4M3 if size == 1 else BF16)
+    cache = Cache(g, [S], G, D, dtype, paged)
+    if paged:
+        blocks = cache.k.shape[0]
+        far = (5 << 30) // size // blocks // 16 * 16       # elements from a block to the next
+        shape, strides = (blocks, G, PAGE, D), (far, PAGE * D, D, 1)
+    else:
+        far = min((5 << 30) // size // cache.capacity // 16 * 16, 1 << 24)     # (the most from a slot to the next)
+        shape, strides = (1, G, cache.capacity, D), (0, D, far, 1)
+    assert far * size * (blocks if paged else cache.capacity) > 1 << 32
+    old = cache.k, cache.v
+    cache.k, cache.v = cells.as_strided(shape, strides, 0), cells.as_strided(shape, strides, 4096)
+    for t, o in zip((cache.k, cache.v), old):
+        as_bytes(t).copy_(as_bytes(o))
+    k, v = normal(g, 1, N, G, D), normal(g, 1, N, G, D)
+    kw = dict(block_table=cache.table, scales=cache.scales)
+    before = [cache.rows64(0, range(P), w) for w in (0, 1)]
+    sv.specvlm_kv_append(k, v, cache.k, cache.v, i32([P]), **kw)
+    for which, x in enumerate((k, v)):
+        want = x[0].double() if dtype == BF16 else (lambda c, e: c * two_to(e)[..., None])(*quantise64(x[0]))
+        assert torch.equal(cache.rows64(0, range(P, S), which), want) and torch.equal(cache.rows64(0, range(P), which), before[which])
+    check_attention(sv, normal(g, 1, N, H, D), cache, [P], [N], parent=random_tree(g, N)[None] if tree else None)
+    for which, x in enumerate(sv.specvlm_kv_read(cache.k, cache.v, i32([S]), S, **kw)):
+        assert torch.equal(x[0].double(), cache.rows64(0, range(S), which))
+
+
+# ---- many requests, many parts, no tokens, no numbers --------------------------------------------
+
+@kinds
+@pytest.mark.parametrize("B", [65, 200])
+@pytest.mark.parametrize("N", [1, 40, 130])
+def test_many_requests(sv, dtype, paged, B, N):
+    """More requests than a wavefront has lanes, some without tokens, some that do not hold."""
+    g = gen(B + N)
+    new = [(7 * b) % (N + 1) for b in range(B)]
+    prefix = [(37 * b) % 50 for b in range(B)]
+    prefix[3], prefix[B - 1], new[B - 1] = 2500, 1700, N
+    cache = Cache(g, [p + n for p, n in zip(prefix, new)], 2, 64, dtype, paged)
+    q = normal(g, B, N, 4, 64)
+    out, lse = check_attention(sv, q, cache, prefix, new)
+    bad_new = list(new)
+    bad_new[5], bad_new[B - 2] = N + 1, -3
+    err, again = i32([0]), torch.full_like(q, 7.0)
+    sv.specvlm_chunk_attn(q, cache.k, cache.v, i32(prefix), num_new=i32(bad_new), block_table=cache.table, scales=cache.scales, out=again, err_flag=err)
+    assert int(err) == 2
+    for b in range(B):
+        if b in (5, B - 2):
+            assert bool((again[b] == 7.0).all())
+        else:
+            # (the bad requests' places go to others, so that keys may be divided otherwise)
+            m = new[b]
+            assert bool((again[b, m:] == 7.0).all())
+            if m:
+                tol = attention64(q, cache, b, prefix[b], m)[2]
+                assert bool(((again[b, :m].double() - out[b, :m].double()).abs() <= 2 * tol).all())
+
+
+@kinds
+def test_one_long_request(sv, dtype, paged):
+    """As many parts of one head's keys as there can be."""
+    g = gen(1)
+    P = 70001
+    cache = Cache(g, [P + 40], 1, 128, dtype, paged)
+    check_attention(sv, normal(g, 1, 1, 4, 128), cache, [P], [1])
+    check_attention(sv, normal(g, 1, 40, 1, 128), cache, [P], [40])
+    check_attention(sv, normal(g, 1, 40, 16, 128), cache, [P], [40])
+
+
+@kinds
+@pytest.mark.parametrize("N", [1, 64, 500])
+def test_no_tokens_at_all(sv, dtype, paged, N):
+    g = gen(N)
+    cache = Cache(g, [40, 0, 3], 2, 128, dtype, paged)
+    q, k = normal(g, 3, N, 8, 128), normal(g, 3, N, 2, 128)
+    held = [as_bytes(t).clone() for t in (cache.k, cache.v)]
+    kw = dict(block_table=cache.table, scales=cache.scales)
+    sv.specvlm_kv_append(k, k, cache.k, cache.v, i32([40, 0, 3]), num_new=i32([0, 0, 0]), **kw)
+    check_attention(sv, q, cache, [40, 0, 3], [0, 0, 0])
+    a, b = sv.specvlm_kv_read(cache.k, cache.v, i32([0, 0, 0]), N, **kw)
+    assert not bool(a.any()) and not bool(b.any())
+    for t, h in zip((cache.k, cache.v), held):
+        assert torch.equal(as_bytes(t).view(torch.uint8), h.view(torch.uint8))
+
+
+@kinds
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_keys_that_are_not_seen_may_be_anything(sv, dtype, paged, value):
+    """The last new token's K is no number (e4m3: a NaN code, whatever it was): the rows that do not see it are what they were, within the bounds of
+    both calls (the reference maximum of a block's rows moves together, also for the row that sees it)."""
+    g = gen(2)
+    for N, tree in ((3, False), (60, True), (300, False)):
+        cache = Cache(g, [100 + N], 2, 128, dtype, paged)
+        q = normal(g, 1, N, 4, 128)
+        parent = random_tree(g, N)[None] if tree else None
+        kw = dict(parent=parent, block_table=cache.table, scales=cache.scales)
+        want = sv.specvlm_chunk_attn(q, cache.k, cache.v, i32([100]), **kw)
+        tol = attention64(q, cache, 0, 100, N, parent)[2]
+        k, v = (cache.rows64(0, [100 + N - 1], w).to(BF16)[None] for w in (0, 1))
+        k.fill_(value)
+        sv.specvlm_kv_append(k, v, cache.k, cache.v, i32([100 + N - 1]), block_table=cache.table, scales=cache.scales)
+        got = sv.specvlm_chunk_attn(q, cache.k, cache.v, i32([100]), **kw)
+        assert bool(((got[0, :-1].double() - want[0, :-1].double()).abs() <= 2 * tol[:-1]).all())

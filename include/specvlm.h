@@ -56,6 +56,7 @@ typedef enum specvlm_dtype {
 
 #define SPECVLM_MAX_NODES 64
 #define SPECVLM_MAX_CHUNK 65536      /* new tokens of a request in one call (specvlm_kv_append, _kv_read, _chunk_attn) */
+#define SPECVLM_MAX_SLOTS (1 << 30)  /* slots of a request's cache or block table in those calls */
 #define SPECVLM_PAGE_SIZE 16
 #define SPECVLM_MAX_SPLITS 64        /* key-range splits per (request, head) */
 #define SPECVLM_COUNTER_STRIDE 32              /* int32 words between the arrival counters of two requests */

@@ -267,6 +267,11 @@ int32_t specvlm_kv_compact_quantized(const specvlm_attn_desc* desc, int32_t L, v
                              err_flag_dev, static_cast<hipStream_t>(stream));
 }
 
+// Slots that the table or the cache has room for: slot numbers, and a tile behind them, stay below 2^31.
+static bool slots_ok(const specvlm_attn_desc& d) {
+    return d.paged ? d.max_blocks_per_req <= SPECVLM_MAX_SLOTS / SPECVLM_PAGE_SIZE : d.kv_capacity <= SPECVLM_MAX_SLOTS;
+}
+
 // New rows into the cache, or cached rows out: what the two calls have in common.
 static int32_t kv_rows(const specvlm_attn_desc* desc, bool append, void* k_cache_dev, void* v_cache_dev,
                        const specvlm_kv_scales* scales, void* k_rows_dev, void* v_rows_dev, int64_t stride_b,
@@ -275,7 +280,7 @@ static int32_t kv_rows(const specvlm_attn_desc* desc, bool append, void* k_cache
     if (!desc || (desc->dtype != SPECVLM_BF16 && desc->dtype != SPECVLM_F32)) return SPECVLM_INVALID_ARG;
     int32_t rc = check_kv_geometry(*desc, scales != nullptr);
     if (rc) return rc;
-    if (desc->N_max < 1 || desc->N_max > SPECVLM_MAX_CHUNK || desc->B > 65535 || desc->H_kv > 65535) return SPECVLM_INVALID_ARG;
+    if (desc->N_max < 1 || desc->N_max > SPECVLM_MAX_CHUNK || desc->B > 65535 || desc->H_kv > 65535 || !slots_ok(*desc)) return SPECVLM_INVALID_ARG;
     if ((desc->paged != 0) != (block_table_dev != nullptr)) return SPECVLM_INVALID_ARG;
     if (!k_cache_dev || !v_cache_dev || !k_rows_dev || !v_rows_dev || !aligned16(k_cache_dev) || !aligned16(v_cache_dev) ||
         !aligned16(k_rows_dev) || !aligned16(v_rows_dev))
@@ -309,7 +314,7 @@ static int32_t check_chunk_desc(const specvlm_attn_desc& d, bool quantised, bool
     if (d.dtype != SPECVLM_BF16) return SPECVLM_INVALID_ARG;
     int32_t rc = check_kv_geometry(d, quantised);
     if (rc) return rc;
-    if (d.H_q < 1 || d.H_q % d.H_kv || d.B > 65535) return SPECVLM_INVALID_ARG;
+    if (d.H_q < 1 || d.H_q % d.H_kv || d.B > 65535 || !slots_ok(d)) return SPECVLM_INVALID_ARG;
     if (d.N_max < 1 || d.N_max > (tree ? SPECVLM_MAX_NODES : SPECVLM_MAX_CHUNK)) return SPECVLM_INVALID_ARG;
     const int64_t group = d.H_q / d.H_kv;
     if (group * (group * d.N_max + 256) >= (int64_t{1} << 31)) return SPECVLM_INVALID_ARG;       // row -> token by a 32-bit reciprocal

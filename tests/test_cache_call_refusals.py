@@ -50,6 +50,8 @@ def test_rows(lib, append):
     assert call(desc(N_max=0)) == INVALID and call(desc(N_max=65537)) == INVALID
     assert call(desc(kv_capacity=0)) == INVALID and call(desc(kv_stride_t=120)) == INVALID and call(desc(kv_stride_h=500 * 128 + 4)) == INVALID
     assert call(desc(kv_stride_b=-8)) == INVALID and call(desc(kv_stride_t=(1 << 24) + 8)) == INVALID
+    assert call(desc(kv_capacity=(1 << 30) + 1)) == INVALID                        # slot numbers and a tile behind them: below 2^31
+    assert call(desc(paged=True, max_blocks_per_req=(1 << 26) + 1), table=FAKE) == INVALID
     assert call(desc(), rows=ODD) == INVALID and call(desc(), cache=ODD) == INVALID
     assert call(desc(), rows=NULL) == INVALID and call(desc(), cache=NULL) == INVALID
     assert call(desc(), strides=(1, 256, 128)) == INVALID and call(desc(), strides=(8, 256, 120)) == INVALID
@@ -93,6 +95,8 @@ def test_attention(lib):
     assert call(desc(H_q=7)) == INVALID and call(desc(H_q=0)) == INVALID and call(desc(D=32)) == INVALID
     assert call(desc(N_max=0)) == INVALID and call(desc(N_max=65537)) == INVALID and call(desc(N_max=65), parent=FAKE) == INVALID
     assert call(desc(H_q=512, N_max=65536)) == INVALID
+    assert call(desc(kv_capacity=(1 << 30) + 1)) == INVALID
+    assert call(desc(paged=True, max_blocks_per_req=(1 << 26) + 1), table=FAKE) == INVALID
     assert call(desc(softmax_scale=-1.0)) == INVALID and call(desc(softmax_scale=float("inf"))) == INVALID
     assert call(desc(softmax_scale=float("nan"))) == INVALID
     assert call(desc(num_splits=2)) == INVALID and call(desc(num_splits=-1)) == INVALID

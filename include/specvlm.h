@@ -554,6 +554,8 @@ int32_t specvlm_kv_compact_quantized(const specvlm_attn_desc *desc, int32_t L,
  * anything; V of the request's visible tokens must be finite for every row that sees them, and V of a new
  * token must be finite (its weight in the rows before it is zero).  Products of bf16 operands (e4m3 values
  * are exact in bf16), fp32 sums and softmax statistics, weights rounded to bf16 for the second product.
+ * The keys of a call are divided among workgroups by all its requests' lengths and parts are added in a fixed order: the
+ * same call gives the same bits; a request in another batch, or with another workspace size, the same within rounding.
  *   desc           dtype SPECVLM_BF16 (SPECVLM_F32: SPECVLM_UNSUPPORTED); N_max 1 .. SPECVLM_MAX_CHUNK, with
  *                  parent 1 .. SPECVLM_MAX_NODES; num_splits 0 lets the library divide the keys, 1 forbids it
  *                  (anything else: SPECVLM_INVALID_ARG); group = H_q / H_kv with group * (group * N_max + 256) < 2^31

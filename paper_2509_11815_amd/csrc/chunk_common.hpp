@@ -156,7 +156,7 @@ __device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& 
     }
     // The least number of rounds a part for which the parts are no more than one workgroup for every place on the chip (or one part an item).
     // Where that leaves places empty because items have few rounds, twice or three times as many shorter parts: kFixed rounds are what a part costs
-    // beside its own (64 rows: 14, four trees over 4864 slots of 40 heads 68 us, with 4 or 8 80 - 86).
+    // beside its own (64 rows: 14, four trees over 4864 slots of 40 heads 67 us, with 4 or 8 80 - 86).
     auto parts_of = [&](int len) __attribute__((always_inline)) {
         int sum = 0;
         for (int b0 = 0; b0 < p.B; b0 += 64) {

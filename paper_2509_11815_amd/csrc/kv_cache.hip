@@ -3,7 +3,7 @@
 // Both are one pass over memory.  A workgroup has the 16 slots that share a page (of a contiguous cache: 16 aligned slots) and four KV
 // heads: one block-table entry, and a head's codes (16 rows, 2 KB at head size 128) and scales (16 bytes) in one piece.  A lane holds 8
 // elements of a row, 16 or 8 lanes a row; every load of a workgroup is on its way before the first is used.  Stores are non-temporal: what a call
-// writes is more than the L2s hold or is next used by another launch (read 26 752 rows of 40 heads 171 -> 154 us, append 8447 of 32 heads in bf16
+// writes is more than the L2s hold or is next used by another launch (read 27 649 rows of 40 heads 171 -> 154 us, append 8447 of 32 heads in bf16
 // 48 -> 41; non-temporal loads lose: of a fused buffer's lines a workgroup takes a part).
 //
 //   quantise  e = smallest whole number with max |x| <= 448 * 2^e, from the bits of the greatest magnitude (lanes of a row meet by DPP).

@@ -408,3 +408,59 @@ def test_keys_that_are_not_seen_may_be_anything(sv, dtype, paged, value):
         sv.specvlm_kv_append(k, v, cache.k, cache.v, i32([100 + N - 1]), block_table=cache.table, scales=cache.scales)
         got = sv.specvlm_chunk_attn(q, cache.k, cache.v, i32([100]), **kw)
         assert bool(((got[0, :-1].double() - want[0, :-1].double()).abs() <= 2 * tol[:-1]).all())
+
+
+# ---- other orders of the queries, the longest chunks ---------------------------------------------
+
+@kinds
+@pytest.mark.parametrize("N,tree", [(1, False), (33, False), (60, True), (400, False)])
+def test_head_major_queries(sv, dtype, paged, N, tree):
+    """Queries and outputs [B, H, N, D], as a transposed view; one request's queries for every request of a batch (stride zero)."""
+    g = gen(N)
+    cache = Cache(g, [150 + N, 20 + N], 2, 128, dtype, paged)
+    parent = torch.stack([random_tree(g, N) for _ in range(2)]) if tree else None
+    q = normal(g, 2, 6, N, 128).transpose(1, 2)
+    out, _ = check_attention(sv, q, cache, [150, 20], [N, N], parent=parent)
+    kw = dict(parent=parent, block_table=cache.table, scales=cache.scales)
+    dense = sv.specvlm_chunk_attn(q.contiguous(), cache.k, cache.v, i32([150, 20]), **kw)
+    assert torch.equal(out, dense)
+    one = q[:1].expand(2, -1, -1, -1)
+    shared = torch.empty_like(q).contiguous()
+    sv.specvlm_chunk_attn(one, cache.k, cache.v, i32([150, 20]), out=shared, **kw)
+    assert torch.equal(shared, sv.specvlm_chunk_attn(one.contiguous(), cache.k, cache.v, i32([150, 20]), **kw))
+
+
+@kinds
+@pytest.mark.parametrize("N,H,G,D,P", [(65536, 1, 1, 64, 0), (65536, 4, 1, 128, 1000), (40000, 32, 32, 64, 37), (9000, 64, 4, 128, 0)])
+def test_longest_chunks(sv, dtype, paged, N, H, G, D, P):
+    """The most tokens a call takes, and more row blocks than a divided call has: some rows against the reference, and all rows written."""
+    g = gen(N + H)
+    S = P + N
+    k, v = normal(g, 1, S, G, D), normal(g, 1, S, G, D)
+    blocks = -(-S // PAGE)
+    table = torch.randperm(blocks, generator=g, device="cuda").to(torch.int32)[None] if paged else None
+    shape = (blocks, G, PAGE, D) if paged else (1, G, S, D)
+    kc, vc = (torch.zeros(shape, dtype=torch.uint8 if dtype == E4M3 else dtype, device="cuda") for _ in range(2))
+    scales = None
+    if dtype == E4M3:
+        kc, vc = kc.view(E4M3), vc.view(E4M3)
+        scales = tuple(torch.zeros(shape[:3], dtype=torch.uint8, device="cuda") for _ in range(2))
+    kw = dict(block_table=table, scales=scales)
+    for at in range(0, S, 65536):                          # (as many rows as a call takes)
+        sv.specvlm_kv_append(k[:, at:at + 65536], v[:, at:at + 65536], kc, vc, i32([at]), **kw)
+    rows = [sv.specvlm_kv_read(kc, vc, i32([min(65536, S - at)]), min(65536, S - at), start=i32([at]), **kw) for at in range(0, S, 65536)]
+    k, v = (torch.cat([r[w] for r in rows], 1)[0] for w in (0, 1))
+
+    class Rows:
+        heads = G
+
+        def rows64(self, b, slots, which):
+            return (k, v)[which][slots.start:slots.stop].double()
+
+    q = normal(g, 1, N, H, D)
+    out = torch.full_like(q, math.nan)
+    sv.specvlm_chunk_attn(q, kc, vc, i32([P]), out=out, **kw)
+    assert bool(torch.isfinite(out).all())
+    for i in (0, 1, 31, 63, 255, 256, N // 3, N // 2 + 17, N - 257, N - 1):
+        o, _, tol, _ = attention64(q[:, i:i + 1], Rows(), 0, P + i, 1)
+        assert bool(((out[0, i:i + 1].double() - o).abs() <= tol).all()), i

@@ -8,7 +8,8 @@
 //   softmax   one pass, the reference maximum moves only where a score lies 2^8 above it; maximum, sum and accumulators in fp32
 //   merge     four wavefronts with a key stream each (tiles of 32 keys, every fourth) meet in LDS, ranges of keys through the workspace
 //
-// Bound by the stream of K and V.  Two workgroups a compute unit: nothing of the next tile is in registers but what has been loaded of it.
+// Bound by the stream of K and V (one token over 131 000 slots of 8 heads 91 us, 5.9 TB/s; sixteen over 64 - 16 383 in e4m3 34 us) and, where that
+// is short, by its chain of latencies (one over 768 slots of 32 heads 10.8 us).  Two workgroups a compute unit: nothing of the next tile is in registers but what has been loaded of it.
 #include "chunk_common.hpp"
 
 namespace specvlm {
@@ -43,7 +44,7 @@ __device__ __forceinline__ void attend32(const ChunkParams& p) {
     unsigned long long anc[1] = {};
     if (p.parent && !ancestors(p, it, lane, rows.token, anc)) return;
     const int first_token = divide(row0, p.magic_group);
-    const int last_token = Work<ChunkParams, 32, false>::last_token(p, n, it.rb);
+    const int last_token = Work<ChunkParams, 32>::last_token(p, n, it.rb);
     const int all_see = p.parent ? P : P + first_token + 1;          // slots that every row of the block sees
     const int end = p.parent ? S : P + last_token + 1;               // slots that some row sees
     // Tiles of this segment, up to the block's end; this wavefront's stream has every fourth.
@@ -278,7 +279,8 @@ ChunkPlan chunk_plan(const specvlm_attn_desc& d, bool tree, size_t bytes) {
     const int64_t most = std::min<int64_t>(!plan.qb ? plan.places : std::max<int64_t>((plan.qb == 1 ? 2 : 3) * plan.places, pairs), slots);
     if (plan.qb && most < pairs) return plan;
     plan.target = static_cast<int>(most);
-    plan.workgroups = (std::max<int64_t>(plan.target, plan.qb ? 0 : pairs) + 7) / 8 * 8;
+    // (shared: stretches, or an item each and one more for every half)
+    plan.workgroups = (std::max<int64_t>(plan.target, plan.qb ? 0 : pairs + plan.target / 2) + 7) / 8 * 8;
     plan.bytes = kChunkCounterBytes + static_cast<size_t>(plan.target) * 2 * part_bytes(block, d.D);
     return plan;
 }

@@ -126,7 +126,7 @@ __device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& 
         }
         if (it.rb * ROWS >= p.group * it.n) return false;
         it.from = 0;
-        it.to = it.steps = Work<ChunkParams, ROWS, false>::rounds(it.P, it.n);
+        it.to = it.steps = Work<ChunkParams, ROWS>::rounds(it.P, it.n);
         return true;
     }
     int n = 0, P = 0, rounds = 0, units = 0;               // of request b0 + lane
@@ -139,8 +139,8 @@ __device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& 
             if (const int err = length_error(p, n, P)) {
                 if (report && p.err_flag) atomicOr(p.err_flag, err);
             } else if (n) {
-                rounds = Work<ChunkParams, ROWS, false>::rounds(P, n);
-                units = Work<ChunkParams, ROWS, false>::blocks(p, n) * p.H_kv;
+                rounds = Work<ChunkParams, ROWS>::rounds(P, n);
+                units = Work<ChunkParams, ROWS>::blocks(p, n) * p.H_kv;
             }
         }
     };
@@ -209,9 +209,9 @@ __device__ __forceinline__ bool find_item(const ChunkParams& p, int lane, Item& 
 }
 
 // Where a workgroup's share begins.  False: nothing to do.
-template <int ROWS, bool TILES>
-__device__ __forceinline__ bool begin_share(Share<ChunkParams, ROWS, TILES>& s, int lane) {
-    using W = Work<ChunkParams, ROWS, TILES>;
+template <int ROWS, bool HALVES>
+__device__ __forceinline__ bool begin_share(Share<ChunkParams, ROWS, HALVES>& s, int lane) {
+    using W = Work<ChunkParams, ROWS>;
     const ChunkParams& p = s.p;
     s.done = false;
     s.skip = 0;
@@ -278,7 +278,12 @@ __device__ __forceinline__ bool begin_share(Share<ChunkParams, ROWS, TILES>& s, 
     }
     if (!items) return false;
     s.divide_line(sum, items, heaviest);
-    if (s.undivided_is_faster(sum, items, heaviest, lightest == heaviest)) return undivided(false);
+    if constexpr (HALVES) {
+        const int halved = s.choose(sum, items, heaviest, lightest == heaviest);
+        if (halved >= 0) return s.whole_item(blockIdx.x, halved);
+    } else {
+        if (s.undivided_is_faster(sum, items, heaviest, lightest == heaviest)) return undivided(false);
+    }
     s.mine = s.stretch_of(blockIdx.x);
     if (s.mine < 0) return false;
     const double at = s.cut(s.mine);
@@ -410,11 +415,11 @@ struct Segments {
     Item item[2];
     int some[2];
 };
-template <int ROWS, bool TILES>
+template <int ROWS, bool HALVES>
 __device__ __forceinline__ bool next_segment(const ChunkParams& p, Segments& lds, int turn, Item& it) {
     const int lane = this_thread() & 63, at = turn & 1;    // (two places: a slow wavefront may still read the last one)
     if (threadIdx.x < 64) {
-        Share<ChunkParams, ROWS, TILES> share(p);
+        Share<ChunkParams, ROWS, HALVES> share(p);
         Item found;
         bool some;
         if (turn) {

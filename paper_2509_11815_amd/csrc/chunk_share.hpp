@@ -44,35 +44,31 @@ SPECVLM_SHARE_FN int chunk_length_error(int n, int P, int N_max, int capacity) {
 struct Item { int b, hk, rb, n, P, from, to, steps, part, parts, first; };
 
 // ---- the division of a call ------------------------------------------------------------------
-// The host does not know the lengths, the device does.  All (request, KV head, row block) items, one after another, are a line of weights (what
-// an item costs); every workgroup has an equal stretch of it, cut at whole steps, and works out from the lengths which items that is.  An item
-// that a cut goes through has several parts, whose results meet in the workspace.  ROWS: rows of a block.  A step is a tile of every key
-// stream (128 keys), or a tile of 32 keys (TILES), where the blocks of a causal chunk differ in their number.
-// Weights are whole numbers and sums of them stay below 2^53 (at most kMostPairs items), so that all workgroups work out the same cuts.
-template <typename Params, int ROWS, bool TILES>
+// The host does not know the lengths, the device does.  What an item is; ROWS: rows of a block.
+template <typename Params, int ROWS>
 struct Work {
-    // What an item costs beside its steps, in steps: first loads, the meeting of the streams, the result
-    static constexpr int kFixed = TILES ? 4 : 3;
-    static constexpr float kLeast = TILES ? 12.f : 3.f;   // weight of a stretch at least, in steps: two cuts of an item lie a step apart or more
     static SPECVLM_SHARE_FN int blocks(const Params& p, int n) { return static_cast<int>((static_cast<uint32_t>(p.group) * n + ROWS - 1) / ROWS); }
+    // Rounds of four key streams: 128 keys
     static SPECVLM_SHARE_FN int rounds(int P, int n) { return static_cast<int>((static_cast<uint32_t>(P + n - 1) + kSharesRound) / kSharesRound); }
     static SPECVLM_SHARE_FN int last_token(const Params& p, int n, int rb) {
         const int last = quotient((rb + 1) * ROWS - 1, p.magic_group);
         return last < n - 1 ? last : n - 1;
     }
-    static SPECVLM_SHARE_FN int steps(const Params& p, int n, int P, int rb) {
-        return TILES ? (P + last_token(p, n, rb)) / kChunkKeys + 1 : rounds(P, n);
-    }
-    // (TILES: in units of 1 / (32 group) tiles, the last block's full)
+    // Shared tiles: a step is a tile of 32 keys.  Weight of an item: its steps and what it costs beside them (first loads, the result), in units
+    // of 1 / (32 group) tiles, the last block's full: whole numbers, sums of which stay below 2^53 (at most kMostPairs items).
+    static constexpr int kFixed = 4;
+    static SPECVLM_SHARE_FN int steps(const Params& p, int n, int P, int rb) { return (P + last_token(p, n, rb)) / kChunkKeys + 1; }
     static SPECVLM_SHARE_FN double weight(const Params& p, int n, int P, int rb) {
-        if constexpr (TILES) return (static_cast<double>(P) + kFixed * kChunkKeys) * p.group + static_cast<double>(ROWS) * (rb + 1);
-        else return rounds(P, n) + kFixed;
+        return (static_cast<double>(P) + kFixed * kChunkKeys) * p.group + static_cast<double>(ROWS) * (rb + 1);
     }
     static SPECVLM_SHARE_FN double before(const Params& p, int n, int P, int rb) {       // of a head's blocks 0 .. rb - 1
-        if constexpr (TILES) return ((static_cast<double>(P) + kFixed * kChunkKeys) * p.group + 0.5 * ROWS * (rb + 1)) * rb;
-        else return (rounds(P, n) + kFixed) * static_cast<double>(rb);
+        return ((static_cast<double>(P) + kFixed * kChunkKeys) * p.group + 0.5 * ROWS * (rb + 1)) * rb;
     }
 };
+
+// Shared tiles.  All (request, KV head, row block) items, one after another, are a line of weights; every workgroup has an equal stretch of
+// it, cut at whole steps, and works out from the lengths which items that is: all of them the same cuts.  An item that a cut goes through has several
+// parts, whose results meet in the workspace.  Or, where that is estimated to be faster, a workgroup has an item, or half of one.
 
 // Where a workgroup is in its share; in LDS while its wavefronts work on a segment.
 struct ShareState {
@@ -82,9 +78,11 @@ struct ShareState {
 };
 
 // A workgroup's share, item by item.  The first wavefront works it out.
-template <typename Params, int ROWS, bool TILES>
+template <typename Params, int ROWS, bool HALVES>
 struct Share {
-    using W = Work<Params, ROWS, TILES>;
+    using W = Work<Params, ROWS>;
+    static constexpr float kLeast = 12.f;                  // steps of a stretch at least, so that two cuts of an item lie a step apart or more
+    static constexpr int kNear = 6, kHalved = 24;          // steps from an end at which a cut is moved there; of an item that is halved at least
     const Params& p;
     double per;                                            // weight of a stretch
     float inv_per;
@@ -92,7 +90,7 @@ struct Share {
     int b, hk, rb, n, P, blocks;                           // item the share is at
     double base;                                           // where its request begins
     int skip;                                              // its first step
-    bool whole;                                            // one item a workgroup, nothing divided
+    bool whole;                                            // an item, or half of one, a workgroup (skip: 1, 2 which; mine: who has the first)
     bool done;
 
     SPECVLM_SHARE_FN Share(const Params& p_) : p(p_) {}
@@ -109,8 +107,7 @@ struct Share {
     // Where in an item that begins at `begin` stretch w's cut is, in steps; near an end it is moved there
     SPECVLM_SHARE_FN int step_at(int w, double begin, float rate, int steps) const {
         const int t = static_cast<int>(static_cast<float>(cut(w) - begin) * rate + 0.5f);
-        const int near = TILES ? 6 : 1;
-        return t < near ? 0 : t > steps - near ? steps : t;
+        return t < kNear ? 0 : t > steps - kNear ? steps : t;
     }
     // The first stretch that begins at x or behind it
     SPECVLM_SHARE_FN int stretch_from(double x) const {
@@ -131,7 +128,7 @@ struct Share {
     // The number of stretches: as many as workgroups fit the chip, but none shorter than kLeast steps, and one each where there are fewer items
     // than that; at most kMostParts of the heaviest item.
     SPECVLM_SHARE_FN void divide_line(double line, int items, float heaviest) {
-        const float total = static_cast<float>(line), least = W::kLeast * (TILES ? kChunkKeys * p.group : 1);
+        const float total = static_cast<float>(line), least = kLeast * kChunkKeys * p.group;
         const float parts = total * reciprocal(heaviest) * (0.9999f * (kMostParts - 2));
         float most = floorf(total * reciprocal(least) * 0.9999f);
         most = most > items ? most : items;
@@ -145,11 +142,53 @@ struct Share {
     // first loads) are about 25 tiles' time: 3008 tokens of 32 heads 92 us undivided, 118 divided; 1024, 1024 and 333 tokens over 4096, 7001 and 5120
     // keys of 8 heads 419 undivided, 258 divided.  Undivided: one round of items takes as long as the longest, more of them about as long as
     // the mean where they begin in the order of their lengths (requests of one length), and up to half an item longer otherwise.
+    SPECVLM_SHARE_FN float undivided_time(double line, int items, float heaviest, bool even) const {
+        const float mean = static_cast<float>(line) * (1.f / 256);
+        const float undivided = items <= 256 ? heaviest : even ? 1.08f * mean : mean + 0.4f * heaviest;
+        return undivided > heaviest ? undivided : heaviest;
+    }
     SPECVLM_SHARE_FN bool undivided_is_faster(double line, int items, float heaviest, bool even) const {
-        const float unit = TILES ? kChunkKeys * p.group : 1, mean = static_cast<float>(line) * (1.f / 256);
-        float undivided = items <= 256 ? heaviest : even ? 1.08f * mean : mean + 0.4f * heaviest;
-        undivided = undivided > heaviest ? undivided : heaviest;
-        return undivided < static_cast<float>(per) + 25.f * unit;
+        return undivided_time(line, items, heaviest, even) < static_cast<float>(per) + 25.f * (kChunkKeys * p.group);
+    }
+    // HALVES: equal stretches (-1), or an item a workgroup with the last k blocks of every head in halves.  A half, whose workgroup has nothing else to
+    // begin, costs about 12 tiles' time: 1024 tokens of 32 heads 37.8 -> 32.0 us, 1536 51.9 -> 40.0; only while all are under way at once, for otherwise
+    // halves take the compute units that other items need (2048 tokens 66 -> 73).  bf16 caches only: with the same code the e4m3 kernel of paged caches
+    // keeps fewer of its scalars in registers (1024 tokens 42 -> 36.6, but 4096 154 -> 164 and chunks of 1024, 1024 and 333 248 -> 260).
+    SPECVLM_SHARE_FN int choose(double line, int items, float heaviest, bool even) const {
+        const float unit = kChunkKeys * p.group, part = 0.5f * heaviest + 12.f * unit;
+        float time = undivided_time(line, items, heaviest, even);
+        int halved = 0;
+        const int pairs = p.B * p.H_kv;
+        for (int k = 1; items + k * pairs <= 256 && 2 * k * pairs <= p.target && k <= p.row_blocks; ++k) {
+            const float rest = heaviest - static_cast<float>(ROWS) * k, t = rest > part ? rest : part;
+            if (t < time) {
+                time = t;
+                halved = k;
+            }
+        }
+        return u(time < static_cast<float>(per) + 25.f * unit ? halved : -1);
+    }
+    // An item a workgroup, every head's longest first, the first `halved` of them in halves.
+    SPECVLM_SHARE_FN bool whole_item(uint32_t workgroup, int halved) {
+        const uint32_t pairs = static_cast<uint32_t>(p.B) * p.H_kv, halves = 2 * halved * pairs;
+        uint32_t level, pair;
+        whole = true;
+        skip = 0;
+        if (workgroup < halves) {
+            level = workgroup / (2 * pairs);
+            pair = (workgroup - level * 2 * pairs) >> 1;
+            skip = u(1 + (workgroup & 1));
+            mine = u(workgroup & ~1u);
+        } else {
+            level = (workgroup - halves) / pairs;
+            pair = workgroup - halves - level * pairs;
+            level += halved;
+        }
+        b = u(pair / static_cast<uint32_t>(p.H_kv));
+        hk = u(pair - b * p.H_kv);
+        if (!lengths(b)) return false;
+        rb = u(blocks - 1 - static_cast<int>(level));
+        return rb >= 0;
     }
     // Stretch number of a workgroup, -1: it has none.  Every XCD has contiguous ones, so that the row blocks of a head's keys share an L2.
     SPECVLM_SHARE_FN int stretch_of(int workgroup) const {
@@ -204,6 +243,17 @@ struct Share {
             it.first = 0;
             if (whole) {
                 done = true;
+                if constexpr (HALVES) {
+                    it.from = 0;
+                    if (skip && it.steps < kHalved) return skip == 1;
+                    if (skip) {
+                        it.part = u(skip - 1);
+                        it.parts = 2;
+                        it.first = mine;
+                        if (it.part) it.from = it.steps >> 1;
+                        else it.to = it.steps >> 1;
+                    }
+                }
                 return true;
             }
             const double weight = W::weight(p, n, P, rb);
